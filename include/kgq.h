@@ -472,6 +472,129 @@ kgq_status kgq_profile_intervals(kgq_handle* h, int32_t stage, double* out, int6
 kgq_status kgq_dense(kgq_handle* h, const float* x, int32_t M, int32_t K, const float* w, const float* b,
                      int32_t N, int32_t act, float* y, void* stream);
 
+/* ---- Drawing from scores, learning from a teacher's lists -----------------
+ * Calls on score matrices (kgq_execute's out_scores, or the caller's own; one
+ * row per query, n_entities columns) and on tables of the caller's. They are
+ * asynchronous on `stream`, use no memory of the handle's and none but their
+ * arguments, may overlap on different streams, and may be captured into a
+ * graph; in checked mode they synchronise the stream and report what they
+ * found, as kgq_execute does, and cannot be captured. dtype is KGQ_F32 or
+ * KGQ_BF16 (bfloat16 bit patterns); strides (ld) are in elements, and rows
+ * need no alignment beyond an element's. */
+
+/* How to draw. Settings hold for every row; where an array (device memory,
+ * [batch], or NULL) is given, row b takes its own from it.
+ *   temperature  scores are divided by it, finite and >= 0; 0 takes the first
+ *                entity in the ranking order (score descending, equal scores by
+ *                index ascending)
+ *   top_k        keep the first top_k entities of that order (0: all)
+ *   top_p        of these, keep the shortest prefix that holds at least this
+ *                share of their weight, > 0 (1 or above: all)
+ *   min_p        of these, keep those of at least this share of the largest
+ *                weight, in [0, 1] */
+typedef struct {
+    float temperature;
+    int32_t top_k;
+    float top_p;
+    float min_p;
+    const float* temperature_rows;
+    const int32_t* top_k_rows;
+    const float* top_p_rows;
+    const float* min_p_rows;
+} kgq_sampling;
+
+/* Draw n_draws entities for each row of scores, with replacement, from given
+ * random numbers: entity i has weight exp((score_i - best) / temperature)
+ * where `how` keeps it, and a draw u takes the first entity by index at which
+ * the running sum of the weights exceeds u times their total.
+ *   scores    device [batch x n_entities], row stride ld. -inf and NaN have no
+ *             weight (masked entities); where the best score is +inf, the
+ *             entities that have it share the weight
+ *   u         device float [batch x n_draws] in [0, 1) (NaN and below: 0; 1 and
+ *             above: the last entity kept)
+ *   out_idx   device int32 [batch x n_draws]; -1 in a row with nothing to draw
+ *             from (every entity masked), or with a setting of its own outside
+ *             its range (INVALID_ARG in checked mode)
+ *   out_logp  device float [batch x n_draws] or NULL: log of the probability
+ *             with which the entity was drawn (NaN where out_idx is -1)
+ * Weights and their sums are in double precision; results are the same in
+ * every call.
+ * Errors: INVALID_ARG (NULL scores, how, u or out_idx, unknown dtype, batch
+ * outside [1, 2^20], n_draws < 1, ld < n_entities, a setting outside its
+ * range; checked mode under capture), NO_DEVICE, DEVICE. */
+kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t dtype, int64_t ld,
+                      const kgq_sampling* how, const float* u, int32_t n_draws, int32_t* out_idx, float* out_logp,
+                      void* stream);
+
+/* Distillation: the loss of a student's scores against a teacher's lists, and
+ * its gradient with respect to the scores, in one pass. With p the softmax of
+ * a list's scores / temperature and q the softmax of the row's scores /
+ * temperature over all entities,
+ *   loss[b]    = temperature^2 sum_j p_j (log p_j - log q[idx_j])
+ *   grad[b][i] = row_weight[b] temperature (q_i - sum of p_j with idx_j = i)
+ * so grad is that of sum_b row_weight[b] loss[b].
+ *   scores         device [batch x n_entities] of dtype, row stride ld
+ *   teacher_idx    device int32 [batch x k], teacher_score device float
+ *                  [batch x k], 1 <= k <= KGQ_MAX_K: lists as kgq_execute's
+ *                  top-k writes them, in any order. Entries with idx -1 are left
+ *                  out (shorter lists), as are ids out of range (OUT_OF_RANGE in
+ *                  checked mode) and scores of -inf. An entity that occurs more
+ *                  than once has the sum of its p
+ *   temperature    finite, > 0
+ *   row_weight     device float [batch], or NULL (1 for every row)
+ *   out_loss       device float [batch] or NULL (without row_weight)
+ *   out_grad       device [batch x n_entities] of dtype, row stride ld_grad, or
+ *                  NULL; may be `scores` itself (with the same stride), and must
+ *                  not overlap it otherwise
+ * A row whose list is empty has loss 0 and gradient 0; a row of weight 0 has
+ * gradient 0. Student scores of -inf have q = 0 (a listed one makes the loss
+ * +inf); a NaN or +inf, a row of -inf alone, or a NaN in the list, makes the
+ * row NaN. Both softmaxes' sums are float32 or wider, the loss is summed in
+ * double precision; a bfloat16 gradient is rounded once. Results are the same
+ * in every call.
+ * Errors: INVALID_ARG (NULL scores or lists, no output, unknown dtype, batch
+ * outside [1, 2^20], a stride below n_entities, k or temperature out of range;
+ * checked mode under capture), OUT_OF_RANGE (checked), NO_DEVICE, DEVICE. */
+kgq_status kgq_distill(kgq_handle* h, int32_t batch, const void* scores, int32_t dtype, int64_t ld, int32_t k,
+                       const int32_t* teacher_idx, const float* teacher_score, float temperature,
+                       const float* row_weight, float* out_loss, void* out_grad, int64_t ld_grad, void* stream);
+
+/* Rows of a table by id: out[t] = scale * table[ids[t]], t = 0 .. n - 1.
+ *   table  device [rows x dim] of dtype, row stride ld
+ *   ids    device int32 [n]; -1 (padding) gives a row of zeros, and so does an
+ *          id outside [0, rows) (OUT_OF_RANGE in checked mode)
+ *   out    device [n x dim] of out_dtype, row stride ld_out; must not overlap
+ *          the table
+ * The product is float32, rounded once for a bfloat16 output. n = 0 does
+ * nothing.
+ * Errors: INVALID_ARG (NULL pointers, unknown dtypes, rows outside [1, 2^31-1],
+ * dim < 1, n < 0, a stride below dim; checked mode under capture),
+ * OUT_OF_RANGE (checked), NO_DEVICE, DEVICE. */
+kgq_status kgq_embed(kgq_handle* h, const void* table, int32_t dtype, int64_t rows, int32_t dim, int64_t ld,
+                     const int32_t* ids, int32_t n, float scale, void* out, int32_t out_dtype, int64_t ld_out,
+                     void* stream);
+
+/* Gradient of kgq_embed with respect to the table: out[v] = scale * sum of
+ * grad[t] over the t with ids[t] = v (added to out[v] if accumulate).
+ *   grad        device [n x dim] of dtype, row stride ld
+ *   ids         device int32 [n], as in kgq_embed: tokens with -1 or an id out
+ *               of range add nothing
+ *   out         device [rows x dim] of out_dtype, row stride ld_out. accumulate
+ *               0: every row is written, zeros where no token has its id;
+ *               otherwise rows without a token are left as they are
+ *   ws          device memory, 16-byte aligned, of at least the bytes that
+ *               kgq_embed_grad_workspace reports; a call owns it until it has
+ *               run, so calls that may overlap need one each
+ * Tokens are sorted by id, and the sums are float32 in one order, whatever the
+ * timing: results are the same in every call. Rounded once for a bfloat16
+ * output.
+ * Errors: as kgq_embed, and INVALID_ARG for a ws that is NULL, not aligned or
+ * too small. */
+kgq_status kgq_embed_grad_workspace(const kgq_handle* h, int64_t rows, int32_t dim, int32_t n, size_t* bytes);
+kgq_status kgq_embed_grad(kgq_handle* h, const void* grad, int32_t dtype, int32_t n, int32_t dim, int64_t ld,
+                          const int32_t* ids, int64_t rows, float scale, void* out, int32_t out_dtype, int64_t ld_out,
+                          int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
 /* Free the handle and everything it owns: parameters, derived tables,
  * compiled plans and scratch (the counterpart of kgq_create). Waits for the
  * handle's work in flight first. NULL is accepted. */

@@ -28,7 +28,7 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I" + os.path
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-result"]
 EXTRA = {"k_score.hip": ["-fno-honor-nans"]}
 SOURCES = ["kgq_api.cpp", "plan.cpp", "k_embed.hip", "k_gemm.hip", "k_score.hip", "k_score_kl.hip", "k_topk.hip",
-           "k_rank.hip", "k_cone_logice.hip"]
+           "k_rank.hip", "k_cone_logice.hip", "k_sample.hip", "k_distill.hip", "k_rows.hip"]
 
 
 def _compile(src: str, verbose: bool) -> str:

@@ -1679,6 +1679,177 @@ kgq_status kgq_dense(kgq_handle* h, const float* x, int32_t M, int32_t K, const 
     return KGQ_OK;
 }
 
+namespace {
+
+// The call's device, current again what it was before at the end.
+struct DeviceGuard {
+    int before = -1;
+    hipError_t enter(int device)
+    {
+        hipError_t e = hipGetDevice(&before);
+        if (e != hipSuccess || before == device) {
+            before = -1;
+            return e;
+        }
+        return hipSetDevice(device);
+    }
+    ~DeviceGuard()
+    {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+// Calls on the caller's own arrays (kgq_sample to kgq_embed_grad) use nothing
+// of the handle's unless it is checked, so they may be captured and may
+// overlap. In checked mode the error bits live in a lane.
+kgq_status rows_begin(kgq_handle* h, DeviceGuard& dev, hipStream_t s, Lane** L)
+{
+    *L = nullptr;
+    if (h->dry) return fail(h, KGQ_E_NO_DEVICE, "validation-only handle (device = -1)");
+    HIP_TRY(h, dev.enter(h->cfg.device));
+    if (!h->checked) return KGQ_OK;
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    HIP_TRY(h, hipStreamIsCapturing(s, &cap));
+    if (cap != hipStreamCaptureStatusNone)
+        return fail(h, KGQ_E_INVALID_ARG, "checked mode synchronises the stream: turn it off to capture the call");
+    kgq_status st = acquire_lane(h, s, L);
+    if (st != KGQ_OK) return st;
+    launch_clear_flag((*L)->dflag, s);
+    return KGQ_OK;
+}
+
+kgq_status rows_end(kgq_handle* h, Lane* L, hipStream_t s, const char* what_range)
+{
+    HIP_TRY(h, hipGetLastError());
+    if (!L) return KGQ_OK;
+    L->done_live = hipEventRecord(L->done, s) == hipSuccess;
+    HIP_TRY(h, hipMemcpyAsync(L->hflag, L->dflag, sizeof(int), hipMemcpyDeviceToHost, s));
+    HIP_TRY(h, hipStreamSynchronize(s));
+    if (*L->hflag & kErrSettings)
+        return fail(h, KGQ_E_INVALID_ARG, "a row's temperature, top_k, top_p or min_p is outside its range");
+    if (*L->hflag & kErrRange) return fail(h, KGQ_E_OUT_OF_RANGE, what_range);
+    return KGQ_OK;
+}
+
+bool is_dtype(int32_t t) { return t == KGQ_F32 || t == KGQ_BF16; }
+constexpr int32_t kMaxRowBatch = 1 << 20;
+
+}  // namespace
+
+kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t dtype, int64_t ld,
+                      const kgq_sampling* how, const float* u, int32_t n_draws, int32_t* out_idx, float* out_logp,
+                      void* stream)
+{
+    if (!h) return KGQ_E_INVALID_ARG;
+    if (!scores || !how || !u || !out_idx)
+        return fail(h, KGQ_E_INVALID_ARG, "scores, how, u and out_idx must not be NULL");
+    if (!is_dtype(dtype)) return fail(h, KGQ_E_INVALID_ARG, "unknown dtype");
+    if (batch < 1 || batch > kMaxRowBatch) return fail(h, KGQ_E_INVALID_ARG, "batch outside [1, 2^20]");
+    if (n_draws < 1) return fail(h, KGQ_E_INVALID_ARG, "n_draws must be >= 1");
+    const int64_t N = h->cfg.n_entities;
+    if (ld < N) return fail(h, KGQ_E_INVALID_ARG, "ld must be >= n_entities");
+    if (!how->temperature_rows && !(how->temperature >= 0.f && how->temperature <= 3.4028234e38f))
+        return fail(h, KGQ_E_INVALID_ARG, "temperature must be finite and >= 0");
+    if (!how->top_k_rows && how->top_k < 0) return fail(h, KGQ_E_INVALID_ARG, "top_k must be >= 0");
+    if (!how->top_p_rows && !(how->top_p > 0.f)) return fail(h, KGQ_E_INVALID_ARG, "top_p must be > 0");
+    if (!how->min_p_rows && !(how->min_p >= 0.f && how->min_p <= 1.f))
+        return fail(h, KGQ_E_INVALID_ARG, "min_p outside [0, 1]");
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    DeviceGuard dev;
+    Lane* L = nullptr;
+    kgq_status st = rows_begin(h, dev, s, &L);
+    if (st != KGQ_OK) return st;
+    launch_sample({scores, dtype, ld, N, batch, n_draws, how->temperature, how->top_k, how->top_p, how->min_p,
+                   how->temperature_rows, how->top_k_rows, how->top_p_rows, how->min_p_rows, u, out_idx, out_logp,
+                   L ? L->dflag : nullptr},
+                  s);
+    return rows_end(h, L, s, "");
+}
+
+kgq_status kgq_distill(kgq_handle* h, int32_t batch, const void* scores, int32_t dtype, int64_t ld, int32_t k,
+                       const int32_t* teacher_idx, const float* teacher_score, float temperature,
+                       const float* row_weight, float* out_loss, void* out_grad, int64_t ld_grad, void* stream)
+{
+    if (!h) return KGQ_E_INVALID_ARG;
+    if (!scores || !teacher_idx || !teacher_score)
+        return fail(h, KGQ_E_INVALID_ARG, "scores, teacher_idx and teacher_score must not be NULL");
+    if (!out_loss && !out_grad) return fail(h, KGQ_E_INVALID_ARG, "no output requested");
+    if (!is_dtype(dtype)) return fail(h, KGQ_E_INVALID_ARG, "unknown dtype");
+    if (batch < 1 || batch > kMaxRowBatch) return fail(h, KGQ_E_INVALID_ARG, "batch outside [1, 2^20]");
+    const int64_t N = h->cfg.n_entities;
+    if (ld < N || (out_grad && ld_grad < N))
+        return fail(h, KGQ_E_INVALID_ARG, "ld and ld_grad must be >= n_entities");
+    if (k < 1 || k > kMaxK) return fail(h, KGQ_E_INVALID_ARG, "k outside [1, KGQ_MAX_K]");
+    if (!(temperature > 0.f && temperature <= 3.4028234e38f))
+        return fail(h, KGQ_E_INVALID_ARG, "temperature must be finite and > 0");
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    DeviceGuard dev;
+    Lane* L = nullptr;
+    kgq_status st = rows_begin(h, dev, s, &L);
+    if (st != KGQ_OK) return st;
+    launch_distill({scores, dtype, ld, N, batch, k, teacher_idx, teacher_score, temperature, row_weight, out_loss,
+                    out_grad, ld_grad, L ? L->dflag : nullptr},
+                   s);
+    return rows_end(h, L, s, "an entity of a teacher's list is out of range");
+}
+
+kgq_status kgq_embed(kgq_handle* h, const void* table, int32_t dtype, int64_t rows, int32_t dim, int64_t ld,
+                     const int32_t* ids, int32_t n, float scale, void* out, int32_t out_dtype, int64_t ld_out,
+                     void* stream)
+{
+    if (!h) return KGQ_E_INVALID_ARG;
+    if (n < 0) return fail(h, KGQ_E_INVALID_ARG, "n must be >= 0");
+    if (!table || (n && (!ids || !out))) return fail(h, KGQ_E_INVALID_ARG, "table, ids and out must not be NULL");
+    if (!is_dtype(dtype) || !is_dtype(out_dtype)) return fail(h, KGQ_E_INVALID_ARG, "unknown dtype");
+    if (rows < 1 || rows > 0x7fffffffLL) return fail(h, KGQ_E_INVALID_ARG, "rows outside [1, 2^31-1]");
+    if (dim < 1) return fail(h, KGQ_E_INVALID_ARG, "dim must be >= 1");
+    if (ld < dim || ld_out < dim) return fail(h, KGQ_E_INVALID_ARG, "ld and ld_out must be >= dim");
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    DeviceGuard dev;
+    Lane* L = nullptr;
+    kgq_status st = rows_begin(h, dev, s, &L);
+    if (st != KGQ_OK) return st;
+    if (n > 0)
+        launch_embed_rows({table, dtype, rows, dim, ld, ids, n, scale, out, out_dtype, ld_out, L ? L->dflag : nullptr},
+                          s);
+    return rows_end(h, L, s, "an id is out of range");
+}
+
+kgq_status kgq_embed_grad_workspace(const kgq_handle* h, int64_t rows, int32_t dim, int32_t n, size_t* bytes)
+{
+    if (!h || !bytes || rows < 1 || rows > 0x7fffffffLL || dim < 1 || n < 0) return KGQ_E_INVALID_ARG;
+    *bytes = (size_t)embed_grad_workspace(n);
+    return KGQ_OK;
+}
+
+kgq_status kgq_embed_grad(kgq_handle* h, const void* grad, int32_t dtype, int32_t n, int32_t dim, int64_t ld,
+                          const int32_t* ids, int64_t rows, float scale, void* out, int32_t out_dtype, int64_t ld_out,
+                          int32_t accumulate, void* ws, size_t ws_bytes, void* stream)
+{
+    if (!h) return KGQ_E_INVALID_ARG;
+    if (n < 0) return fail(h, KGQ_E_INVALID_ARG, "n must be >= 0");
+    if (!out || !ws || (n && (!ids || !grad)))
+        return fail(h, KGQ_E_INVALID_ARG, "grad, ids, out and ws must not be NULL");
+    if (!is_dtype(dtype) || !is_dtype(out_dtype)) return fail(h, KGQ_E_INVALID_ARG, "unknown dtype");
+    if (rows < 1 || rows > 0x7fffffffLL) return fail(h, KGQ_E_INVALID_ARG, "rows outside [1, 2^31-1]");
+    if (dim < 1) return fail(h, KGQ_E_INVALID_ARG, "dim must be >= 1");
+    if (ld < dim || ld_out < dim) return fail(h, KGQ_E_INVALID_ARG, "ld and ld_out must be >= dim");
+    if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(h, KGQ_E_INVALID_ARG, "ws must be 16-byte aligned");
+    const int64_t need = embed_grad_workspace(n);
+    if (ws_bytes < (size_t)need)
+        return fail(h, KGQ_E_INVALID_ARG, "ws holds fewer than the " + std::to_string(need) +
+                                              " bytes of kgq_embed_grad_workspace");
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    DeviceGuard dev;
+    Lane* L = nullptr;
+    kgq_status st = rows_begin(h, dev, s, &L);
+    if (st != KGQ_OK) return st;
+    launch_embed_grad({grad, dtype, n, dim, ld, ids, rows, scale, out, out_dtype, ld_out, accumulate, ws,
+                       L ? L->dflag : nullptr},
+                      s);
+    return rows_end(h, L, s, "an id is out of range");
+}
+
 kgq_status kgq_set_dense_path(kgq_handle* h, int32_t path)
 {
     if (!h) return KGQ_E_INVALID_ARG;

@@ -116,6 +116,7 @@ inline bool mlp_model(int model) { return model == KGQ_BETAE || model == KGQ_CON
 constexpr int kErrRange = 1;    // an anchor or relation id outside its table
 constexpr int kErrPadding = 2;  // a mixed-batch unused slot that is not -1
 constexpr int kErrAnswers = 4;  // an answer list longer than kMaxAnswers or of negative length
+constexpr int kErrSettings = 8; // a row's temperature, top-k, top-p or min-p outside its range
 
 // Largest answer list of one query for the ranking metrics (sorted in LDS).
 constexpr int kMaxAnswers = 1024;
@@ -474,5 +475,50 @@ struct TopkArgs {
 // scratch buffers and they are missing.
 bool launch_topk(const TopkArgs& a, hipStream_t s);
 int64_t topk_scratch_elems(int64_t n_rows, int64_t N, int k);
+
+// ---- drawing, distillation, embedding rows (k_sample, k_distill, k_rows) ----
+// flag: device error bits, or nullptr (not checked).
+
+constexpr int kSampleThreads = 1024;
+
+struct SampleArgs {
+    const void* scores; int dtype; int64_t ld; int64_t N;
+    int batch, S;
+    float temperature; int32_t top_k; float top_p, min_p;        // every row's, where the arrays below are nullptr
+    const float* temperature_rows; const int32_t* top_k_rows; const float* top_p_rows; const float* min_p_rows;
+    const float* u;                    // [batch x S]
+    int32_t* idx; float* logp;         // [batch x S]; logp or nullptr
+    int* flag;
+};
+void launch_sample(const SampleArgs& a, hipStream_t s);
+
+struct DistillArgs {
+    const void* scores; int dtype; int64_t ld; int64_t N;
+    int batch, k;
+    const int32_t* idx; const float* teacher;                    // [batch x k]
+    float tau; const float* weight;    // [batch] or nullptr (1)
+    float* loss;                       // [batch] or nullptr
+    void* grad; int64_t ld_grad;       // of dtype, or nullptr
+    int* flag;
+};
+void launch_distill(const DistillArgs& a, hipStream_t s);
+
+struct EmbedArgs {
+    const void* table; int dtype; int64_t rows; int d; int64_t ld;
+    const int32_t* ids; int n; float scale;
+    void* out; int out_dtype; int64_t ld_out;
+    int* flag;
+};
+void launch_embed_rows(const EmbedArgs& a, hipStream_t s);
+
+struct EmbedGradArgs {
+    const void* grad; int dtype; int n; int d; int64_t ld;
+    const int32_t* ids; int64_t rows; float scale;
+    void* out; int out_dtype; int64_t ld_out; int accumulate;
+    void* ws;                          // embed_grad_workspace bytes
+    int* flag;
+};
+int64_t embed_grad_workspace(int64_t n);
+void launch_embed_grad(const EmbedGradArgs& a, hipStream_t s);
 
 }  // namespace kgq

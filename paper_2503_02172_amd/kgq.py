@@ -52,6 +52,12 @@ class Config(ctypes.Structure):
                 ("concurrency", ctypes.c_int32), ("tnorm", ctypes.c_int32)]
 
 
+class Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float), ("temperature_rows", ctypes.c_void_p), ("top_k_rows", ctypes.c_void_p),
+                ("top_p_rows", ctypes.c_void_p), ("min_p_rows", ctypes.c_void_p)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -86,6 +92,12 @@ def lib() -> ctypes.CDLL:
         "kgq_memory": ([vp, i64p, i64p], i32),
         "kgq_rank_answers": ([vp, i32, vp, i64, vp, vp, vp, vp, vp, vp], i32),
         "kgq_dense": ([vp, vp, i32, i32, vp, vp, i32, i32, vp, vp], i32),
+        "kgq_sample": ([vp, i32, vp, i32, i64, ctypes.POINTER(Sampling), vp, i32, vp, vp, vp], i32),
+        "kgq_distill": ([vp, i32, vp, i32, i64, i32, vp, vp, ctypes.c_float, vp, vp, vp, i64, vp], i32),
+        "kgq_embed": ([vp, vp, i32, i64, i32, i64, vp, i32, ctypes.c_float, vp, i32, i64, vp], i32),
+        "kgq_embed_grad_workspace": ([vp, i64, i32, i32, ctypes.POINTER(ctypes.c_size_t)], i32),
+        "kgq_embed_grad": ([vp, vp, i32, i32, i32, i64, vp, i64, ctypes.c_float, vp, i32, i64, i32, vp,
+                            ctypes.c_size_t, vp], i32),
         "kgq_profile_enable": ([vp, i32], i32),
         "kgq_profile_read": ([vp, i32, dp, i64p], i32),
         "kgq_profile_reset": ([vp], i32),
@@ -340,6 +352,162 @@ class Engine:
         self._check(lib().kgq_dense(self.h, _ptr(x), M, K, _ptr(w), _ptr(b), N, act, _ptr(y),
                                     _stream(stream)))
         return y
+
+    # -- drawing, distillation, embedding rows ----------------------------------
+    def _rows_stream(self, stream, inputs):
+        """The call's torch stream; inputs' memory outlives the work on it."""
+        import torch
+        dev = torch.device("cuda", self.device)
+        if stream is None:
+            return torch.cuda.current_stream(dev)
+        ts = torch.cuda.ExternalStream(stream, device=dev) if isinstance(stream, int) else stream
+        for t in inputs:
+            if t is not None:
+                t.record_stream(ts)
+        return ts
+
+    def _matrix(self, call: str, name: str, t, width: Optional[int] = None):
+        """(dtype, row stride) of a float32 or bfloat16 matrix on the handle's device."""
+        import torch
+        dt = {torch.float32: F32, torch.bfloat16: BF16}.get(t.dtype)
+        if dt is None or t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise TypeError(f"{call}: {name} must be a float32 or bfloat16 CUDA matrix with unit column stride")
+        if t.device.index != self.device:
+            raise ValueError(f"{call}: {name} is not on the handle's device")
+        if width is not None and t.shape[1] != width:
+            raise ValueError(f"{call}: {name} must have {width} columns")
+        # (the stride of a single row is never used)
+        return dt, t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+    def _array(self, call: str, name: str, t, dtype, shape):
+        if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+            raise TypeError(f"{call}: {name} must be a contiguous {str(dtype).split('.')[-1]} CUDA tensor")
+        if t.device.index != self.device:
+            raise ValueError(f"{call}: {name} is not on the handle's device")
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{call}: {name} must have shape {tuple(shape)}")
+
+    def sample(self, scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logp: bool = True, stream=None):
+        """kgq_sample: draw u.shape[1] entities for each row of scores [B x N]
+        (float32 or bfloat16) from random numbers u [B x S] float32 in [0, 1).
+        temperature, top_k, top_p and min_p are numbers, or device tensors [B]
+        (float32; top_k int32) with each row's own. Returns (idx int32 [B x S],
+        -1 where a row leaves nothing to draw from; log-probabilities float32
+        [B x S] or None)."""
+        import torch
+        dt, ld = self._matrix("sample", "scores", scores, self.n_entities)
+        B = scores.shape[0]
+        if u.dim() != 2:
+            raise ValueError("sample: u must be [B x S]")
+        self._array("sample", "u", u, torch.float32, (B, u.shape[1]))
+        how = Sampling(1.0, 0, 1.0, 0.0)
+        kept = [scores, u]
+        for name, value in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
+            if torch.is_tensor(value):
+                self._array("sample", name, value, torch.int32 if name == "top_k" else torch.float32, (B,))
+                setattr(how, name + "_rows", _ptr(value))
+                kept.append(value)
+            else:
+                setattr(how, name, value)
+        ts = self._rows_stream(stream, kept)
+        with torch.cuda.stream(ts):
+            idx = torch.empty(u.shape, dtype=torch.int32, device=u.device)
+            lp = torch.empty(u.shape, dtype=torch.float32, device=u.device) if logp else None
+        self._check(lib().kgq_sample(self.h, B, _ptr(scores), dt, ld, ctypes.byref(how), _ptr(u), u.shape[1],
+                                     _ptr(idx), _ptr(lp), _stream(ts)))
+        return idx, lp
+
+    def distill(self, scores, idx, score, temperature: float = 1.0, weight=None, loss: bool = True,
+                grad: bool = True, out=None, stream=None):
+        """kgq_distill: loss [B] float32 of student scores [B x N] (float32 or
+        bfloat16) against a teacher's lists idx [B x k] int32 and score [B x k]
+        float32 (as execute returns them), and the gradient of sum(weight *
+        loss) with respect to scores, of their dtype (into out if given; out
+        may be scores). Returns (loss or None, gradient or None)."""
+        import torch
+        dt, ld = self._matrix("distill", "scores", scores, self.n_entities)
+        B = scores.shape[0]
+        if idx.dim() != 2:
+            raise ValueError("distill: idx must be [B x k]")
+        self._array("distill", "idx", idx, torch.int32, (B, idx.shape[1]))
+        self._array("distill", "score", score, torch.float32, (B, idx.shape[1]))
+        if weight is not None:
+            self._array("distill", "weight", weight, torch.float32, (B,))
+        ld_grad = 0
+        if out is not None:
+            odt, ld_grad = self._matrix("distill", "out", out, self.n_entities)
+            if odt != dt or out.shape[0] != B:
+                raise ValueError("distill: out must have the shape and dtype of scores")
+            same = out.data_ptr() == scores.data_ptr() and ld_grad == ld
+            end = [t.data_ptr() + ((B - 1) * s + self.n_entities) * t.element_size() for t, s in
+                   ((scores, ld), (out, ld_grad))]
+            if not same and out.data_ptr() < end[0] and scores.data_ptr() < end[1]:
+                raise ValueError("distill: out overlaps scores and is not the same matrix")
+        ts = self._rows_stream(stream, (scores, idx, score, weight, out))
+        with torch.cuda.stream(ts):
+            ls = torch.empty(B, dtype=torch.float32, device=scores.device) if loss else None
+            if grad and out is None:
+                out = torch.empty((B, self.n_entities), dtype=scores.dtype, device=scores.device)
+                ld_grad = self.n_entities
+        g = out if grad else None
+        self._check(lib().kgq_distill(self.h, B, _ptr(scores), dt, ld, idx.shape[1], _ptr(idx), _ptr(score),
+                                      temperature, _ptr(weight), _ptr(ls), _ptr(g), ld_grad, _stream(ts)))
+        return ls, g
+
+    def embed(self, table, ids, scale: float = 1.0, dtype=None, stream=None):
+        """kgq_embed: scale * table[ids] for a table [V x d] (float32 or
+        bfloat16) and int32 ids of any shape; -1 gives zeros. Returns a tensor
+        ids.shape + (d,) of dtype (the table's by default)."""
+        import torch
+        dt, ld = self._matrix("embed", "table", table)
+        self._array("embed", "ids", ids, torch.int32, None)
+        d = table.shape[1]
+        dtype = dtype or table.dtype
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("embed: dtype must be float32 or bfloat16")
+        ts = self._rows_stream(stream, (table, ids))
+        with torch.cuda.stream(ts):
+            out = torch.empty(tuple(ids.shape) + (d,), dtype=dtype, device=table.device)
+        self._check(lib().kgq_embed(self.h, _ptr(table), dt, table.shape[0], d, ld, _ptr(ids), ids.numel(), scale,
+                                    _ptr(out), F32 if dtype == torch.float32 else BF16, d, _stream(ts)))
+        return out
+
+    def embed_grad(self, grad, ids, rows: int, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False,
+                   stream=None):
+        """kgq_embed_grad: the gradient of embed with respect to its table of
+        `rows` rows, from grad (ids.shape + (d,), float32 or bfloat16). Returns
+        a tensor [rows x d] of dtype (float32 by default), or out, which
+        accumulate adds to."""
+        import torch
+        self._array("embed_grad", "ids", ids, torch.int32, None)
+        if tuple(grad.shape[:-1]) != tuple(ids.shape):
+            raise ValueError("embed_grad: grad must have shape ids.shape + (d,)")
+        if grad.dim() != 2:
+            grad = grad.reshape(-1, grad.shape[-1])
+        dt, ld = self._matrix("embed_grad", "grad", grad)
+        n, d = grad.shape
+        if accumulate and out is None:
+            raise ValueError("embed_grad: accumulate needs out")
+        if out is not None:
+            odt, ld_out = self._matrix("embed_grad", "out", out, d)
+            if out.shape[0] != rows or (dtype is not None and dtype != out.dtype):
+                raise ValueError("embed_grad: out must be [rows x d] of dtype")
+        else:
+            dtype = dtype or torch.float32
+            if dtype not in (torch.float32, torch.bfloat16):
+                raise TypeError("embed_grad: dtype must be float32 or bfloat16")
+            odt, ld_out = (F32 if dtype == torch.float32 else BF16), d
+        need = ctypes.c_size_t()
+        if lib().kgq_embed_grad_workspace(self.h, rows, d, n, ctypes.byref(need)) != OK:
+            raise ValueError("embed_grad: rows, d or the number of ids is out of range")
+        ts = self._rows_stream(stream, (grad, ids, out))
+        with torch.cuda.stream(ts):
+            if out is None:
+                out = torch.empty((rows, d), dtype=dtype, device=grad.device)
+            ws = torch.empty(need.value, dtype=torch.uint8, device=grad.device)
+        self._check(lib().kgq_embed_grad(self.h, _ptr(grad), dt, n, d, ld, _ptr(ids), rows, scale, _ptr(out), odt,
+                                         ld_out, int(accumulate), _ptr(ws), need.value, _stream(ts)))
+        return out
 
     # -- profiling ------------------------------------------------------------
     def profile(self, stages=None):

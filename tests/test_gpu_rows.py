@@ -1,0 +1,270 @@
+"""Embedding rows and their gradient (kgq_embed, kgq_embed_grad) against the
+definitions in 64 bits, and the operators together: a student's step."""
+
+import numpy as np
+import pytest
+
+from paper_2503_02172_amd import kgq
+from tests import rows_ref as R
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": "float32", "bf16": "bfloat16"}
+
+
+@pytest.fixture(scope="module")
+def eng():
+    e = kgq.Engine(kgq.GQE, 16, 1, 4, 24.0, 1)
+    yield e
+    e.close()
+
+
+def dev(a, dtype="f32"):
+    import torch
+    return torch.as_tensor(a, device="cuda").to(getattr(torch, DT[dtype])) if dtype else torch.as_tensor(a, device="cuda")
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def ids_of(n, V, seed):
+    """Log-uniform ids (a few take much of the use) and some padding."""
+    rng = np.random.default_rng(seed)
+    ids = np.minimum(np.exp(rng.random(n) * np.log(V)) - 1, V - 1).astype(np.int32)
+    ids = ((ids.astype(np.int64) * 7919) % V).astype(np.int32)
+    ids[rng.random(n) < 0.05] = -1
+    return ids
+
+
+SIZES = [(1, 1, 1), (5, 3, 7), (64, 40, 64), (300, 1000, 33), (14505, 61, 400), (1000, 5000, 16), (50, 3001, 130),
+         (70000, 9, 100), (7, 2049, 1601), (300, 20000, 5)]
+
+
+@pytest.mark.parametrize("src,out", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("V,n,d", SIZES)
+def test_gpu_embed(eng, V, n, d, src, out):
+    import torch
+    rng = np.random.default_rng(V + n)
+    for pad in (0, 1, 4, 5):
+        t = dev(rng.normal(0, 1, (V, d + pad)), src)[:, pad:]           # rows at odd elements too
+        ids = ids_of(n, V, d)
+        got = host(eng.embed(t, dev(ids, None), scale=1.7, dtype=getattr(torch, DT[out])))
+        ref = np.where(ids[:, None] >= 0, host(t)[np.maximum(ids, 0)] * float(np.float32(1.7)), 0.0)
+        bound = R.U32 * np.abs(ref) * 1.01 + (R.U16 * np.abs(ref) * 1.01 if out == "bf16" else 0)
+        assert (np.abs(got - ref) <= bound).all(), pad
+        if src == out:
+            assert np.array_equal(host(eng.embed(t, dev(ids, None))), np.where(ids[:, None] >= 0,
+                                                                             host(t)[np.maximum(ids, 0)], 0.0))
+
+
+@pytest.mark.parametrize("src,out", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("V,n,d", SIZES)
+def test_gpu_embed_grad(eng, V, n, d, src, out):
+    import torch
+    rng = np.random.default_rng(V + n)
+    for pad in (0, 1, 4):
+        g = dev(rng.normal(0, 1, (n, d + pad)), src)[:, pad:]
+        ids = ids_of(n, V, d)
+        base = dev(rng.normal(0, 1, (V, d + pad)), out)[:, pad:]
+        ti = dev(ids, None)
+        got = eng.embed_grad(g, ti, V, scale=0.7, dtype=getattr(torch, DT[out]))
+        ref, bound = R.embed_grad(host(g), ids, V, float(np.float32(0.7)))
+        extra = (lambda r, b: R.U16 * (np.abs(r) + b)) if out == "bf16" else (lambda r, b: 0.0)
+        assert (np.abs(host(got) - ref) <= bound + extra(ref, bound)).all(), pad
+        assert torch.equal(got, eng.embed_grad(g, ti, V, scale=0.7, dtype=getattr(torch, DT[out])))
+        old = host(base)
+        ref, bound = R.embed_grad(host(g), ids, V, float(np.float32(0.7)), old)
+        acc = eng.embed_grad(g, ti, V, scale=0.7, out=base, accumulate=True)
+        assert acc is base
+        assert (np.abs(host(acc) - ref) <= bound + extra(ref, bound)).all(), pad
+        unused = np.setdiff1d(np.arange(V), ids)
+        assert np.array_equal(host(acc)[unused], old[unused])           # left as they were
+
+
+@pytest.mark.parametrize("V", [3, 255, 256, 300, 65535, 65536, 70001])
+def test_gpu_embed_grad_id_ranges(eng, V):
+    """Tables whose ids end below, at and above a byte; the last id; one id
+    alone; no token; padding alone; ids out of range."""
+    rng = np.random.default_rng(V)
+    for n in (1, 2, 300, 2048, 2049, 9000):
+        for kind in ("random", "last", "one", "padding", "outside", "descending"):
+            ids = rng.integers(0, V, n).astype(np.int32)
+            if kind == "last":
+                ids[:] = V - 1
+            elif kind == "one":
+                ids[:] = V // 2
+            elif kind == "padding":
+                ids[:] = -1
+            elif kind == "outside":
+                ids[::2] = np.resize([V, -2, 2 ** 31 - 1, -2 ** 31], ids[::2].size)
+            elif kind == "descending":
+                ids = np.sort(ids)[::-1].copy()
+            g = rng.normal(0, 1, (n, 6)).astype(np.float32)
+            got = host(eng.embed_grad(dev(g), dev(ids, None), V))
+            ref, bound = R.embed_grad(g, ids, V, 1.0)
+            assert (np.abs(got - ref) <= bound).all(), (n, kind)
+
+
+def test_gpu_embed_empty(eng):
+    import torch
+    t = torch.ones(5, 8, device="cuda")
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert eng.embed(t, none).shape == (0, 8)
+    g = torch.zeros(0, 8, device="cuda")
+    assert torch.equal(eng.embed_grad(g, none, 5), torch.zeros(5, 8, device="cuda"))
+    assert torch.equal(eng.embed_grad(g, none, 5, out=t, accumulate=True), torch.ones(5, 8, device="cuda"))
+    ids = torch.tensor([[1, 2], [4, -1]], dtype=torch.int32, device="cuda")
+    assert eng.embed(t, ids).shape == (2, 2, 8)
+    assert eng.embed_grad(eng.embed(t, ids), ids, 5)[:, 0].tolist() == [0, 1, 1, 0, 1]
+
+
+def test_gpu_embed_values_that_are_not_finite(eng):
+    import torch
+    t = torch.tensor([[1.0, float("nan")], [float("inf"), -0.0], [2.0, 3.0]], device="cuda")
+    ids = torch.tensor([0, 1, -1, 2, 1], dtype=torch.int32, device="cuda")
+    got = eng.embed(t, ids, scale=2.0)
+    assert got[0, 0] == 2 and got[0, 1].isnan() and got[1, 0] == float("inf") and (got[2] == 0).all()
+    g = torch.zeros(5, 2, device="cuda")
+    g[2] = float("nan")                                        # padding's gradient is not read into anything
+    g[1, 0] = float("inf")
+    d = eng.embed_grad(g, ids, 3)
+    assert d[1, 0] == float("inf") and d.isnan().sum() == 0
+
+
+def test_gpu_embed_checked_mode():
+    import torch
+    e = kgq.Engine(kgq.GQE, 16, 1, 4, 24.0, 1)
+    t = torch.ones(10, 8, device="cuda")
+    good, bad = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, -1, 9], [0, 10, 3]))
+    assert (e.embed(t, bad)[1] == 0).all()                     # not checked: zeros
+    e.set_checked(True)
+    e.embed(t, good)
+    e.embed_grad(t[:3], good, 10)
+    for call in (lambda: e.embed(t, bad), lambda: e.embed_grad(t[:3], bad, 10)):
+        with pytest.raises(kgq.KgqError) as ei:
+            call()
+        assert ei.value.name == "OUT_OF_RANGE"
+    e.embed(t, good)
+    e.close()
+
+
+def test_gpu_embed_offsets_past_32_bits(eng):
+    import torch
+    V, d, ld = 70000, 40, 32768
+    t = torch.empty(V, ld, dtype=torch.bfloat16, device="cuda")[:, :d]
+    use = torch.tensor([0, 65535, 65536, 69999, 65537], device="cuda")
+    t[use] = torch.randn(5, d, device="cuda").bfloat16()
+    got = eng.embed(t, use.int())
+    assert torch.equal(got, t[use])
+    g = torch.randn(5, d, device="cuda")
+    old = torch.zeros(5, d, device="cuda").bfloat16()
+    t[use] = old
+    eng.embed_grad(g, use.int(), V, out=t, accumulate=True)
+    assert torch.equal(t[use], g.bfloat16())
+
+
+def test_gpu_embed_grad_is_the_adjoint(eng):
+    """<g, embed(T)> = <embed_grad(g), T>: the lookup is linear in the table."""
+    rng = np.random.default_rng(2)
+    V, n, d = 300, 4000, 24
+    t, g, ids = rng.normal(0, 1, (V, d)), rng.normal(0, 1, (n, d)), ids_of(n, V, 3)
+    a = (g.astype(np.float32) * host(eng.embed(dev(t), dev(ids, None), scale=3.0))).sum()
+    b = (host(eng.embed_grad(dev(g), dev(ids, None), V, scale=3.0)) * t.astype(np.float32)).sum()
+    assert abs(a - b) < 1e-5 * np.abs(g).sum()
+
+
+def test_gpu_embed_streams_and_graphs(eng):
+    """Two captured graphs of the pair with a workspace each, eager calls
+    between the replays, and a call on another stream."""
+    import torch
+    V, n, d = 3000, 5000, 48
+    t = torch.randn(V, d, device="cuda")
+    ids = dev(ids_of(n, V, 1), None)
+    g = torch.randn(n, d, device="cuda")
+    eng.embed(t, ids)
+    eng.embed_grad(g, ids, V)
+    torch.cuda.synchronize()
+    graphs = []
+    for scale in (1.0, 2.5):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            out = eng.embed(t, ids, scale=scale), eng.embed_grad(g, ids, V, scale=scale)
+        graphs.append((scale, gr, out))
+    for turn in range(3):
+        t.normal_()
+        g.normal_()
+        ids.copy_(dev(ids_of(n, V, 10 + turn), None))
+        for scale, gr, out in graphs:
+            eager = eng.embed(t, ids, scale=scale), eng.embed_grad(g, ids, V, scale=scale)
+            gr.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out[0], eager[0]) and torch.equal(out[1], eager[1]), (turn, scale)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for stream in (s, s.cuda_stream):
+        a, b = eng.embed(t, ids, stream=stream), eng.embed_grad(g, ids, V, stream=stream)
+        s.synchronize()
+        assert torch.equal(a, eng.embed(t, ids)) and torch.equal(b, eng.embed_grad(g, ids, V))
+
+
+def test_gpu_embed_binding_refusals(eng):
+    import torch
+    t = torch.zeros(10, 8, device="cuda")
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    g = torch.zeros(4, 8, device="cuda")
+    for call in (lambda: eng.embed(t, ids.long()), lambda: eng.embed(t.half(), ids), lambda: eng.embed(t.t(), ids),
+                 lambda: eng.embed(t, ids, dtype=torch.float16), lambda: eng.embed(t, ids.cpu()),
+                 lambda: eng.embed_grad(g.half(), ids, 10), lambda: eng.embed_grad(g, ids, 10, dtype=torch.int32)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: eng.embed_grad(g[:3], ids, 10), lambda: eng.embed_grad(g, ids, 0),
+                 lambda: eng.embed_grad(g, ids, 10, accumulate=True), lambda: eng.embed_grad(g, ids, 9, out=t),
+                 lambda: eng.embed_grad(g[:, :7], ids, 10, out=t)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_gpu_a_students_step():
+    """The operators as they are used together: a teacher's execute gives
+    lists; a student's query rows are embeddings of the anchors plus those of
+    the relations, its scores their products with its entity table; the loss
+    against the lists, and its gradient back to both tables, against
+    differences of the loss in 64 bits. Negatives are drawn from the student's
+    scores, and their rows looked up."""
+    import torch
+    from oracle import oracle as O
+    from paper_2503_02172_amd import synth
+    N, NR, d, B, K = 700, 9, 32, 24, 20
+    wl = synth.make_tiny(O.GQE, n_ent=N, n_rel=NR, dim=16, seed=3)
+    qb = synth.draw_queries("1p", B, N, NR, seed=4)
+    rng = np.random.default_rng(5)
+    E, Rel = rng.normal(0, 0.5, (N, d)), rng.normal(0, 0.5, (NR, d))
+    anchors, rels = (np.ascontiguousarray(x[:, 0], np.int32) for x in (qb.anchors, qb.relations))
+    w = np.full(B, 1.0 / B)
+    with kgq.engine_for(wl, max_batch=B) as eng:
+        top = eng.execute(synth.STRUCTURE_ID["1p"], qb.anchors, qb.relations, k=K)
+        tE, tR, ta, tr = dev(E), dev(Rel), dev(anchors, None), dev(rels, None)
+        q = eng.embed(tE, ta) + eng.embed(tR, tr)
+        s = eng.dense(q, tE)
+        loss, ds = eng.distill(s, top["idx"], top["score"], temperature=2.0, weight=dev(w))
+        dq = ds @ tE
+        dE = ds.t().contiguous() @ q
+        eng.embed_grad(dq, ta, N, out=dE, accumulate=True)
+        dR = eng.embed_grad(dq, tr, NR)
+        negatives, logp = eng.sample(s, torch.rand(B, 7, device="cuda"), temperature=2.0, min_p=1e-6)
+        rows = eng.embed(tE, negatives)
+        idx, sc = top["idx"].cpu().numpy(), top["score"].cpu().numpy()
+        assert torch.equal(rows, tE[negatives.long()]) and (logp <= 0).all()
+
+    def total(E_, R_):
+        z = (E_[anchors] + R_[rels]) @ E_.T
+        return (w * R.distill(z, idx, sc, 2.0, w)[0]).sum()
+    assert abs((w * host(loss)).sum() - total(E, Rel)) < 1e-4 * total(E, Rel)
+    h = 1e-5
+    for _ in range(3):
+        vE, vR = rng.normal(0, 1, E.shape), rng.normal(0, 1, Rel.shape)
+        diff = (total(E + h * vE, Rel + h * vR) - total(E - h * vE, Rel - h * vR)) / (2 * h)
+        mine = (host(dE) * vE).sum() + (host(dR) * vR).sum()
+        # products of 32 to 700 float32 terms, 24 bits each
+        assert abs(diff - mine) < 1e-4 * (np.abs(host(dE) * vE).sum() + np.abs(host(dR) * vR).sum())
