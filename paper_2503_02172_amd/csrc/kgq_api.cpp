@@ -1818,7 +1818,7 @@ kgq_status kgq_embed(kgq_handle* h, const void* table, int32_t dtype, int64_t ro
 kgq_status kgq_embed_grad_workspace(const kgq_handle* h, int64_t rows, int32_t dim, int32_t n, size_t* bytes)
 {
     if (!h || !bytes || rows < 1 || rows > 0x7fffffffLL || dim < 1 || n < 0) return KGQ_E_INVALID_ARG;
-    *bytes = (size_t)embed_grad_workspace(n);
+    *bytes = (size_t)embed_grad_workspace(n, dim);
     return KGQ_OK;
 }
 
@@ -1835,7 +1835,7 @@ kgq_status kgq_embed_grad(kgq_handle* h, const void* grad, int32_t dtype, int32_
     if (dim < 1) return fail(h, KGQ_E_INVALID_ARG, "dim must be >= 1");
     if (ld < dim || ld_out < dim) return fail(h, KGQ_E_INVALID_ARG, "ld and ld_out must be >= dim");
     if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(h, KGQ_E_INVALID_ARG, "ws must be 16-byte aligned");
-    const int64_t need = embed_grad_workspace(n);
+    const int64_t need = embed_grad_workspace(n, dim);
     if (ws_bytes < (size_t)need)
         return fail(h, KGQ_E_INVALID_ARG, "ws holds fewer than the " + std::to_string(need) +
                                               " bytes of kgq_embed_grad_workspace");

@@ -518,7 +518,7 @@ struct EmbedGradArgs {
     void* ws;                          // embed_grad_workspace bytes
     int* flag;
 };
-int64_t embed_grad_workspace(int64_t n);
+int64_t embed_grad_workspace(int64_t n, int d);
 void launch_embed_grad(const EmbedGradArgs& a, hipStream_t s);
 
 }  // namespace kgq
