@@ -19,38 +19,113 @@ namespace {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortParts = kSortThreads / 256;
+constexpr int kSortBlocks = 128;             // blocks of a pass at most
 constexpr int kSortShort = 4096;             // tokens that the counting sort takes
-constexpr int kJoinWaves = 8;
+constexpr int kJoinWaves = 16;
+constexpr int kJoinAhead = 16;               // pieces in flight per wavefront
+constexpr int kJoinAlone = 32;               // pieces of a run that one wavefront adds
 constexpr int kAhead = 8;                    // gradient rows in flight per group
 constexpr int kFillRows = 16;                // table rows per wavefront that are looked up for zeros
 
 }  // namespace
 
-// ---- lookup -----------------------------------------------------------------
-
-template <typename T, typename O>
-__global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs a)
+// Elements at p and the row's end `left` columns on (more or fewer than V).
+template <int V, typename T>
+__device__ __forceinline__ void load_columns(const T* p, int left, float (&x)[V])
 {
-    const int64_t total = (int64_t)a.n * a.d;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t t = i / a.d, c = i % a.d;
-        const int32_t id = a.ids[t];
-        const bool ok = id >= 0 && id < a.rows;
-        if (!ok && id != -1 && a.flag) atomicOr(a.flag, kErrRange);
-        const float x = ok ? a.scale * row_value(reinterpret_cast<const T*>(a.table)[id * a.ld + c]) : 0.f;
-        reinterpret_cast<O*>(a.out)[t * a.ld_out + c] = row_element<O>(x);
+    typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    if (left >= V) {
+        const vec v = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = row_value((T)v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = j < left ? row_value(p[j]) : 0.f;
+    }
+}
+// p[j] = scale x[j] (+ p[j])
+template <int V, typename O>
+__device__ __forceinline__ void store_columns(O* p, int left, const float (&x)[V], float scale, bool accumulate)
+{
+    typedef O vec __attribute__((ext_vector_type(V), aligned(sizeof(O))));
+    if (left >= V) {
+        vec old = {}, y;
+        if (accumulate) old = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            y[j] = row_element<O>(accumulate ? x[j] * scale + row_value((O)old[j]) : x[j] * scale);
+        *reinterpret_cast<vec*>(p) = y;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j < left) p[j] = row_element<O>(accumulate ? x[j] * scale + row_value(p[j]) : x[j] * scale);
     }
 }
 
+// ---- lookup -----------------------------------------------------------------
+
+// A workgroup takes `per` tokens, whose rows of `vecs` vectors of V elements
+// lie one after the other over its threads: U vectors a thread, all of them
+// loaded before the first is stored. inv = 2^32 / vecs rounded up: a quotient
+// below 2^32 / vecs by one multiplication.
+template <typename T, typename O, int U>
+__global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs a, int per, int vecs, uint32_t inv)
+{
+    constexpr int V = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4;
+    const int64_t t0 = (int64_t)blockIdx.x * per;
+    const T* table = reinterpret_cast<const T*>(a.table);
+    O* out = reinterpret_cast<O*>(a.out);
+    for (int j0 = threadIdx.x; j0 < per * vecs; j0 += U * 256) {
+        float x[U][V];
+        int64_t t[U];
+        int c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * 256;
+            const int r = per == 1 ? 0 : vecs == 1 ? j : (int)__umulhi((uint32_t)j, inv);
+            t[u] = t0 + r;
+            c[u] = (j - r * vecs) * V;
+            if (j >= per * vecs || t[u] >= a.n) t[u] = -1;
+            const int32_t id = t[u] >= 0 ? a.ids[t[u]] : -1;
+            if (id >= 0 && id < a.rows) {
+                load_columns<V>(table + (int64_t)id * a.ld + c[u], a.d - c[u], x[u]);
+            } else {
+                if (id != -1 && a.flag) atomicOr(a.flag, kErrRange);
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[u][i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t[u] >= 0) store_columns<V>(out + t[u] * a.ld_out + c[u], a.d - c[u], x[u], a.scale, false);
+    }
+}
+
+namespace {
+
+template <typename T, typename O>
+void launch_embed(const EmbedArgs& a, hipStream_t s)
+{
+    constexpr int V = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4;
+    const int vecs = (a.d + V - 1) / V;
+    // four vectors a thread where that still leaves two workgroups a compute
+    // unit; one where latency counts
+    const bool many = (int64_t)a.n * vecs >= (int64_t)512 * 1024;
+    const int per = std::max(1, (many ? 1024 : 256) / vecs);
+    const uint32_t inv = (uint32_t)(((1ull << 32) + vecs - 1) / vecs);
+    const dim3 grid((uint32_t)(((int64_t)a.n + per - 1) / per));
+    if (many) hipLaunchKernelGGL((k_embed_rows<T, O, 4>), grid, dim3(256), 0, s, a, per, vecs, inv);
+    else hipLaunchKernelGGL((k_embed_rows<T, O, 1>), grid, dim3(256), 0, s, a, per, vecs, inv);
+}
+
+}  // namespace
+
 void launch_embed_rows(const EmbedArgs& a, hipStream_t s)
 {
-    const int64_t blocks = std::min<int64_t>(((int64_t)a.n * a.d + 255) / 256, 8192);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(256), 0, s, a); };
-    if (a.dtype == KGQ_F32 && a.out_dtype == KGQ_F32) go(k_embed_rows<float, float>);
-    else if (a.dtype == KGQ_F32) go(k_embed_rows<float, uint16_t>);
-    else if (a.out_dtype == KGQ_F32) go(k_embed_rows<uint16_t, float>);
-    else go(k_embed_rows<uint16_t, uint16_t>);
+    if (a.dtype == KGQ_F32 && a.out_dtype == KGQ_F32) launch_embed<float, float>(a, s);
+    else if (a.dtype == KGQ_F32) launch_embed<float, uint16_t>(a, s);
+    else if (a.out_dtype == KGQ_F32) launch_embed<uint16_t, float>(a, s);
+    else launch_embed<uint16_t, uint16_t>(a, s);
 }
 
 // ---- tokens sorted by id ----------------------------------------------------
@@ -66,29 +141,31 @@ __device__ __forceinline__ uint32_t token_key(const EmbedGradArgs& a, int64_t i)
 
 // Few tokens: a token's place is the number of tokens with a smaller key, or
 // the same key and earlier. One launch; n^2 comparisons, spread over the chip
-// (64 tokens per workgroup, each wavefront against a quarter of all).
-__global__ __launch_bounds__(256) void k_sort_short(EmbedGradArgs a, int32_t* keys_out, int32_t* tokens_out)
+// (64 tokens per workgroup, each of 16 wavefronts against its share of all).
+__global__ __launch_bounds__(kSortThreads) void k_sort_short(EmbedGradArgs a, int32_t* keys_out, int32_t* tokens_out)
 {
     __shared__ alignas(16) uint32_t key[kSortShort];
-    __shared__ uint32_t before[4][64];
+    __shared__ uint32_t before[kSortWaves][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n4 = (a.n + 15) / 16 * 16;
-    for (int i = tid; i < n4; i += 256) key[i] = i < a.n ? token_key(a, i) : ~0u;
+    const int padded = (a.n + 4 * kSortWaves - 1) / (4 * kSortWaves) * (4 * kSortWaves);
+    for (int i = tid; i < padded; i += kSortThreads) key[i] = i < a.n ? token_key(a, i) : ~0u;
     __syncthreads();
     const int t = blockIdx.x * 64 + lane;
     const uint32_t mine = t < a.n ? key[t] : 0u;
     uint32_t count = 0;
-    const int part = n4 / 4, lo = wave * part;
+    const int part = padded / kSortWaves, lo = wave * part;
 #pragma unroll 4
     for (int j = lo; j < lo + part; j += 4) {
         const uint4 k = *reinterpret_cast<const uint4*>(&key[j]);
-        count += (k.x < mine || (k.x == mine && j < t)) + (k.y < mine || (k.y == mine && j + 1 < t)) +
-                 (k.z < mine || (k.z == mine && j + 2 < t)) + (k.w < mine || (k.w == mine && j + 3 < t));
+        count += (k.x < mine + (j < t)) + (k.y < mine + (j + 1 < t)) + (k.z < mine + (j + 2 < t)) +
+                 (k.w < mine + (j + 3 < t));
     }
     before[wave][lane] = count;
     __syncthreads();
     if (wave == 0 && t < a.n) {
-        const uint32_t at = before[0][lane] + before[1][lane] + before[2][lane] + before[3][lane];
+        uint32_t at = 0;
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) at += before[w][lane];
         keys_out[at] = (int32_t)mine;
         tokens_out[at] = t;
     }
@@ -118,29 +195,38 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(EmbedGradArgs a, co
 {
     __shared__ uint32_t base[256];                   // where the block's next key of a digit goes
     __shared__ uint32_t waves[kSortWaves][256];      // a tile's keys of a digit, by wavefront
-    __shared__ uint32_t part[2][kSortParts][256];
+    __shared__ uint4 part[2][kSortWaves][64];        // by wavefront: keys of four digits a lane
     __shared__ uint32_t scan[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     {
-        // each digit's keys, and those in the blocks before this one
-        const int digit = tid & 255, q = tid >> 8;
-        uint32_t all = 0, before = 0;
-#pragma unroll 8
-        for (int b = q; b < (int)gridDim.x; b += kSortParts) {
-            const uint32_t h = hist[(int64_t)b * 256 + digit];
-            all += h;
-            before += b < (int)blockIdx.x ? h : 0u;
-        }
-        part[0][q][digit] = all;
-        part[1][q][digit] = before;
-        __syncthreads();
-        uint32_t x = 0;
-        if (tid < 256) {
-            all = before = 0;
+        // each digit's keys, and those in the blocks before this one: a
+        // wavefront per block's histogram, 16 loads at most, all in flight
+        uint4 all4 = make_uint4(0, 0, 0, 0), before4 = all4;
 #pragma unroll
-            for (int p = 0; p < kSortParts; ++p) {
-                all += part[0][p][tid];
-                before += part[1][p][tid];
+        for (int k = 0; k < kSortBlocks / kSortWaves; ++k) {
+            const int b = k * kSortWaves + wave;
+            if (b < (int)gridDim.x) {
+                const uint4 h = reinterpret_cast<const uint4*>(hist)[(int64_t)b * 64 + lane];
+                const uint32_t take = b < (int)blockIdx.x ? ~0u : 0u;
+                all4.x += h.x;
+                all4.y += h.y;
+                all4.z += h.z;
+                all4.w += h.w;
+                before4.x += h.x & take;
+                before4.y += h.y & take;
+                before4.z += h.z & take;
+                before4.w += h.w & take;
+            }
+        }
+        part[0][wave][lane] = all4;
+        part[1][wave][lane] = before4;
+        __syncthreads();
+        uint32_t x = 0, all = 0, before = 0;
+        if (tid < 256) {
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                all += reinterpret_cast<const uint32_t*>(part[0][w])[tid];
+                before += reinterpret_cast<const uint32_t*>(part[1][w])[tid];
             }
             x = all;
 #pragma unroll
@@ -172,7 +258,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(EmbedGradArgs a, co
         }
         const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
 #pragma unroll
-        for (int w = 0; w < kSortWaves; w += kSortParts) waves[w + (tid >> 8)][tid & 255] = 0;
+        for (int w = 0; w < kSortWaves; w += kSortThreads / 256) waves[w + (tid >> 8)][tid & 255] = 0;
         __syncthreads();
         if (in && rank == 0) waves[wave][digit] = (uint32_t)__popcll(same);
         __syncthreads();
@@ -206,54 +292,6 @@ struct GradCut {
     int chunk, chunks;                               // tokens per chunk, chunks
 };
 
-// n elements at p, from a row whose columns from p on number `left` (more or
-// fewer than n).
-template <typename T>
-__device__ __forceinline__ void load_columns(const T* p, int left, float (&x)[RowVec<T>::n])
-{
-    constexpr int V = RowVec<T>::n;
-    if (left >= V) {
-        const typename RowVec<T>::type v = *reinterpret_cast<const typename RowVec<T>::type*>(p);
-#pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = row_value((T)v[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = j < left ? row_value(p[j]) : 0.f;
-    }
-}
-template <int V, typename O>
-__device__ __forceinline__ void store_row(O* p, int left, const float (&x)[V], float scale, bool accumulate)
-{
-    typedef O vec __attribute__((ext_vector_type(V), aligned(sizeof(O))));
-    if (left >= V) {
-        vec old = {}, y;
-        if (accumulate) old = *reinterpret_cast<const vec*>(p);
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            y[j] = row_element<O>(accumulate ? x[j] * scale + row_value((O)old[j]) : x[j] * scale);
-        *reinterpret_cast<vec*>(p) = y;
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (j < left) p[j] = row_element<O>(accumulate ? x[j] * scale + row_value(p[j]) : x[j] * scale);
-    }
-}
-template <int V>
-__device__ __forceinline__ void store_piece(float* p, int left, const float (&x)[V])
-{
-    typedef float vec __attribute__((ext_vector_type(V), aligned(4)));
-    if (left >= V) {
-        vec y;
-#pragma unroll
-        for (int j = 0; j < V; ++j) y[j] = x[j];
-        *reinterpret_cast<vec*>(p) = y;
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (j < left) p[j] = x[j];
-    }
-}
-
 // First position in keys[0 .. n) with a key of at least v.
 __device__ __forceinline__ int lower_bound(const int32_t* keys, int n, uint32_t v)
 {
@@ -269,7 +307,7 @@ __device__ __forceinline__ int lower_bound(const int32_t* keys, int n, uint32_t 
 // The first `sum_blocks` workgroups sum chunks; the others write zeros to the
 // rows without a token. piece: two rows of sums per chunk, of the run that
 // came from the chunk before and of the run that leaves into the next.
-template <typename T, typename O>
+template <typename T, typename O, bool WIDE>
 __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cut, int sum_blocks, const int32_t* keys,
                                                      const int32_t* tokens, float* piece)
 {
@@ -289,17 +327,18 @@ __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cu
                 constexpr int VO = RowVec<O>::n;
                 for (int c = lane * VO; c < a.d; c += 64 * VO) {
                     const float zero[VO] = {};
-                    store_row<VO>(row + c, a.d - c, zero, 1.f, false);
+                    store_columns<VO>(row + c, a.d - c, zero, 1.f, false);
                 }
             }
         }
         return;
     }
-    const int64_t group = ((int64_t)blockIdx.x * 256 + threadIdx.x) / cut.lanes;
+    int64_t group = ((int64_t)blockIdx.x * 256 + threadIdx.x) / cut.lanes;
+    if (WIDE) group = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t chunk = group / cut.blocks;
     const int col = ((int)(group % cut.blocks) * cut.lanes + (threadIdx.x & (cut.lanes - 1))) * V;
-    const int left = a.d - col;
-    if (chunk >= cut.chunks || left <= 0) return;
+    const int left = a.d - col;                      // (up to 0 in a row's last lanes, which then only keep up)
+    if (chunk >= cut.chunks) return;
     const int lo = (int)(chunk * cut.chunk), hi = (int)min((int64_t)a.n, (chunk + 1) * cut.chunk);
     const T* g = reinterpret_cast<const T*>(a.grad) + col;
     O* out = reinterpret_cast<O*>(a.out) + col;
@@ -309,24 +348,38 @@ __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cu
     auto flush = [&](bool leaves) {
         if ((int64_t)run < a.rows) {
             if (from_before || leaves) {
-                store_piece<V>(piece + (2 * chunk + (from_before ? 0 : 1)) * a.d + col, left, sum);
+                store_columns<V>(piece + (2 * chunk + (from_before ? 0 : 1)) * a.d + col, left, sum, 1.f, false);
             } else {
-                store_row<V>(out + (int64_t)run * a.ld_out, left, sum, a.scale, a.accumulate != 0);
+                store_columns<V>(out + (int64_t)run * a.ld_out, left, sum, a.scale, a.accumulate != 0);
             }
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[j] = 0.f;
         from_before = false;
     };
+    // a whole wavefront per group: its chunk's keys and tokens in one load, then
+    // from lane to scalar register
+    uint32_t keys_ahead = 0, tokens_ahead = 0;
+    if (WIDE && lo + (int)(threadIdx.x & 63) < hi) {
+        keys_ahead = (uint32_t)keys[lo + (threadIdx.x & 63)];
+        tokens_ahead = (uint32_t)tokens[lo + (threadIdx.x & 63)];
+    }
     for (int i0 = lo; i0 < hi; i0 += kAhead) {
         float x[kAhead][V];
         uint32_t key[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int i = min(i0 + u, hi - 1);
-            key[u] = (uint32_t)keys[i];
+            int64_t token;
+            if (WIDE) {
+                key[u] = __builtin_amdgcn_readlane(keys_ahead, i - lo);
+                token = __builtin_amdgcn_readlane(tokens_ahead, i - lo);
+            } else {
+                key[u] = (uint32_t)keys[i];
+                token = tokens[i];
+            }
             // (rows of tokens without an id are not read)
-            if ((int64_t)key[u] < a.rows) load_columns(g + (int64_t)tokens[i] * a.ld, left, x[u]);
+            if ((int64_t)key[u] < a.rows) load_columns<V>(g + token * a.ld, left, x[u]);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -344,61 +397,90 @@ __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cu
     flush(hi < a.n && (uint32_t)keys[hi] == run);
 }
 
-// Block c: if a run starts in chunk c and continues in the next, the sum of
-// its pieces in chunk order (each wavefront adds a share of them, the shares
-// are added in order).
+// Pieces [lo, hi) of a run behind its first one, 256 columns: added to sum.
+__device__ __forceinline__ void add_pieces(const float* rest, int d, int lo, int hi, int col, int left, float (&sum)[4])
+{
+    for (int i = lo; i < hi; i += kJoinAhead) {
+        float x[kJoinAhead][4];
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u)
+            load_columns<4>(rest + (int64_t)2 * min(i + u, hi - 1) * d + col, left, x[u]);
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] += i + u < hi ? x[u][j] : 0.f;
+    }
+}
+
+// The runs that start in one chunk and continue in the next: the sum of their
+// pieces in chunk order. A wavefront looks at one chunk and adds a run of few
+// pieces by itself; the workgroup then takes the longer runs of its 16 chunks
+// together (each wavefront a share of the pieces, the shares added in order).
 template <typename O>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_grad_join(EmbedGradArgs a, GradCut cut, const int32_t* keys,
                                                                const float* piece)
 {
     constexpr int V = 4;
     __shared__ float share[kJoinWaves][64 * V];
+    __shared__ int pieces[kJoinWaves];               // of a run for the workgroup, or 0
+    __shared__ uint32_t ids[kJoinWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = blockIdx.x;
-    const int64_t next = (c + 1) * cut.chunk;        // (chunks but the last one are whole)
-    const uint32_t run = (uint32_t)keys[next - 1];
-    if ((uint32_t)keys[next] != run || (int64_t)run >= a.rows) return;
-    // did it come from the chunk before?
-    if (c > 0 && (uint32_t)keys[next - cut.chunk] == run && (uint32_t)keys[next - cut.chunk - 1] == run) return;
-    const int end = lower_bound(keys, a.n, run + 1);
-    const int n = (int)((end - 1) / cut.chunk - c);  // pieces in the chunks behind this one
-    const int per = (n + kJoinWaves - 1) / kJoinWaves;
-    const int lo = min(n, wave * per), hi = min(n, lo + per);
-    const float* first = piece + (2 * c + 1) * a.d;  // the run's start
-    const float* rest = piece + 2 * (c + 1) * a.d;   // its piece in the next chunk; the others 2 rows on each
-    O* out = reinterpret_cast<O*>(a.out) + (int64_t)run * a.ld_out;
-    for (int col0 = 0; col0 < a.d; col0 += 64 * V) {
-        const int col = col0 + lane * V, left = a.d - col;
-        float sum[V] = {};
-        if (left > 0) {
-            if (wave == 0) load_columns(first + col, left, sum);
-            int i = lo;
-            for (; i + kAhead <= hi; i += kAhead) {
-                float x[kAhead][V];
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) load_columns(rest + (int64_t)2 * (i + u) * a.d + col, left, x[u]);
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) sum[j] += x[u][j];
-            }
-            for (; i < hi; ++i) {
-                float x[V];
-                load_columns(rest + (int64_t)2 * i * a.d + col, left, x);
-#pragma unroll
-                for (int j = 0; j < V; ++j) sum[j] += x[j];
-            }
+    const int64_t c = (int64_t)blockIdx.x * kJoinWaves + wave;
+    int n = 0;                                       // pieces in the chunks behind c
+    uint32_t run = 0;
+    if (c + 1 < cut.chunks) {
+        const int64_t next = (c + 1) * cut.chunk;    // (chunks but the last one are whole)
+        run = (uint32_t)keys[next - 1];
+        bool mine = (uint32_t)keys[next] == run && (int64_t)run < a.rows;
+        // (not if it came from the chunk before)
+        if (mine && c > 0) mine = (uint32_t)keys[next - cut.chunk] != run || (uint32_t)keys[next - cut.chunk - 1] != run;
+        // the chunks behind c that begin with it, 64 at a look
+        for (int64_t k = c + 1; mine; k += 64) {
+            const uint64_t miss = __builtin_amdgcn_ballot_w64(!(k + lane < cut.chunks &&
+                                                                (uint32_t)keys[(k + lane) * cut.chunk] == run));
+            n += miss ? __builtin_ctzll(miss) : 64;
+            mine = miss == 0;
         }
-#pragma unroll
-        for (int j = 0; j < V; ++j) share[wave][lane * V + j] = sum[j];
-        __syncthreads();
-        if (wave == 0 && left > 0) {
-            for (int w = 1; w < kJoinWaves; ++w)
-#pragma unroll
-                for (int j = 0; j < V; ++j) sum[j] += share[w][lane * V + j];
-            store_row<V>(out + col, left, sum, a.scale, a.accumulate != 0);
+    }
+    if (lane == 0) {
+        pieces[wave] = n > kJoinAlone ? n : 0;
+        ids[wave] = run;
+    }
+    if (n > 0 && n <= kJoinAlone) {
+        O* out = reinterpret_cast<O*>(a.out) + (int64_t)run * a.ld_out;
+        for (int col = lane * V; col < a.d; col += 64 * V) {
+            float sum[V];
+            load_columns<V>(piece + (2 * c + 1) * a.d + col, a.d - col, sum);
+            add_pieces(piece + 2 * (c + 1) * a.d, a.d, 0, n, col, a.d - col, sum);
+            store_columns<V>(out + col, a.d - col, sum, a.scale, a.accumulate != 0);
         }
-        __syncthreads();
+    }
+    __syncthreads();
+    for (int r = 0; r < kJoinWaves; ++r) {
+        n = pieces[r];
+        if (n == 0) continue;
+        const int64_t cr = (int64_t)blockIdx.x * kJoinWaves + r;
+        const int per = (n + kJoinWaves - 1) / kJoinWaves;
+        const int lo = min(n, wave * per), hi = min(n, lo + per);
+        O* out = reinterpret_cast<O*>(a.out) + (int64_t)ids[r] * a.ld_out;
+        for (int col0 = 0; col0 < a.d; col0 += 64 * V) {
+            const int col = col0 + lane * V, left = a.d - col;
+            float sum[V] = {};
+            if (left > 0) {
+                if (wave == 0) load_columns<V>(piece + (2 * cr + 1) * a.d + col, left, sum);
+                add_pieces(piece + 2 * (cr + 1) * a.d, a.d, lo, hi, col, left, sum);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) share[wave][lane * V + j] = sum[j];
+            __syncthreads();
+            if (wave == 0 && left > 0) {
+                for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) sum[j] += share[w][lane * V + j];
+                store_columns<V>(out + col, left, sum, a.scale, a.accumulate != 0);
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -406,11 +488,11 @@ namespace {
 
 int64_t align256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Blocks of a sort pass, each over a run of whole tiles: at most 256, so that
-// summing the blocks' histograms stays small beside the pass.
+// Blocks of a sort pass, each over a run of whole tiles: few enough that every
+// block sums the histograms of all.
 int sort_blocks(int64_t n)
 {
-    return (int)std::max<int64_t>(1, std::min<int64_t>(256, (n + kSortThreads - 1) / kSortThreads));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(kSortBlocks, (n + kSortThreads - 1) / kSortThreads));
 }
 
 // Groups of just enough lanes for a row, 16 bytes a lane, and chunks that give
@@ -437,11 +519,16 @@ void launch_grad(const EmbedGradArgs& a, const int32_t* keys, const int32_t* tok
     const int64_t sum_blocks = ((int64_t)cut.chunks * cut.blocks * cut.lanes + 255) / 256;
     const int64_t fill_blocks =
         a.accumulate ? 0 : std::min<int64_t>((a.rows + 4 * kFillRows - 1) / (4 * kFillRows), 1 << 18);
-    if (sum_blocks + fill_blocks > 0)
-        hipLaunchKernelGGL((k_grad_chunks<T, O>), dim3((uint32_t)(sum_blocks + fill_blocks)), dim3(256), 0, s, a, cut,
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)(sum_blocks + fill_blocks)), dim3(256), 0, s, a, cut,
                            (int)sum_blocks, keys, tokens, piece);
+    };
+    if (sum_blocks + fill_blocks > 0) {
+        if (cut.lanes == 64) go(k_grad_chunks<T, O, true>);
+        else go(k_grad_chunks<T, O, false>);
+    }
     if (cut.chunks > 1)
-        hipLaunchKernelGGL(k_grad_join<O>, dim3(cut.chunks - 1), dim3(64 * kJoinWaves), 0, s, a, cut, keys, piece);
+        hipLaunchKernelGGL(k_grad_join<O>, dim3((cut.chunks - 1 + kJoinWaves - 1) / kJoinWaves), dim3(64 * kJoinWaves), 0, s, a, cut, keys, piece);
 }
 
 }  // namespace
@@ -479,7 +566,7 @@ void launch_embed_grad(const EmbedGradArgs& a, hipStream_t s)
             side ^= 2;
         }
     } else if (a.n > 0) {
-        hipLaunchKernelGGL(k_sort_short, dim3((a.n + 63) / 64), dim3(256), 0, s, a, buf[0], buf[1]);
+        hipLaunchKernelGGL(k_sort_short, dim3((a.n + 63) / 64), dim3(kSortThreads), 0, s, a, buf[0], buf[1]);
     }
     if (a.dtype == KGQ_F32 && a.out_dtype == KGQ_F32) launch_grad<float, float>(a, keys, tokens, piece, s);
     else if (a.dtype == KGQ_F32) launch_grad<float, uint16_t>(a, keys, tokens, piece, s);
