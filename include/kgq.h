@@ -503,6 +503,10 @@ typedef struct {
     const float* min_p_rows;
 } kgq_sampling;
 
+/* Device bytes of workspace for a kgq_sample of this batch (0 for n_entities
+ * above 2^23). Errors: INVALID_ARG (NULL argument, batch outside [1, 2^20]). */
+kgq_status kgq_sample_workspace(const kgq_handle* h, int32_t batch, size_t* bytes);
+
 /* Draw n_draws entities for each row of scores, with replacement, from given
  * random numbers: entity i has weight exp((score_i - best) / temperature)
  * where `how` keeps it, and a draw u takes the first entity by index at which
@@ -517,14 +521,17 @@ typedef struct {
  *             its range (INVALID_ARG in checked mode)
  *   out_logp  device float [batch x n_draws] or NULL: log of the probability
  *             with which the entity was drawn (NaN where out_idx is -1)
+ *   ws        device memory, 16-byte aligned, of at least the bytes that
+ *             kgq_sample_workspace reports; a call owns it until it has run, so
+ *             calls that may overlap need one each
  * Weights and their sums are in double precision; results are the same in
  * every call.
  * Errors: INVALID_ARG (NULL scores, how, u or out_idx, unknown dtype, batch
  * outside [1, 2^20], n_draws < 1, ld < n_entities, a setting outside its
- * range; checked mode under capture), NO_DEVICE, DEVICE. */
+ * range, ws NULL, not aligned or too small; checked mode under capture), NO_DEVICE, DEVICE. */
 kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t dtype, int64_t ld,
                       const kgq_sampling* how, const float* u, int32_t n_draws, int32_t* out_idx, float* out_logp,
-                      void* stream);
+                      void* ws, size_t ws_bytes, void* stream);
 
 /* Distillation: the loss of a student's scores against a teacher's lists, and
  * its gradient with respect to the scores, in one pass. With p the softmax of

@@ -1731,14 +1731,31 @@ kgq_status rows_end(kgq_handle* h, Lane* L, hipStream_t s, const char* what_rang
     return KGQ_OK;
 }
 
+kgq_status check_workspace(kgq_handle* h, const void* ws, size_t ws_bytes, int64_t need)
+{
+    if (need > 0 && !ws) return fail(h, KGQ_E_INVALID_ARG, "ws must not be NULL");
+    if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(h, KGQ_E_INVALID_ARG, "ws must be 16-byte aligned");
+    if (ws_bytes < (size_t)need)
+        return fail(h, KGQ_E_INVALID_ARG,
+                    "ws holds fewer than the " + std::to_string(need) + " bytes that the call needs");
+    return KGQ_OK;
+}
+
 bool is_dtype(int32_t t) { return t == KGQ_F32 || t == KGQ_BF16; }
 constexpr int32_t kMaxRowBatch = 1 << 20;
 
 }  // namespace
 
+kgq_status kgq_sample_workspace(const kgq_handle* h, int32_t batch, size_t* bytes)
+{
+    if (!h || !bytes || batch < 1 || batch > kMaxRowBatch) return KGQ_E_INVALID_ARG;
+    *bytes = (size_t)sample_workspace(batch, h->cfg.n_entities);
+    return KGQ_OK;
+}
+
 kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t dtype, int64_t ld,
                       const kgq_sampling* how, const float* u, int32_t n_draws, int32_t* out_idx, float* out_logp,
-                      void* stream)
+                      void* ws, size_t ws_bytes, void* stream)
 {
     if (!h) return KGQ_E_INVALID_ARG;
     if (!scores || !how || !u || !out_idx)
@@ -1754,13 +1771,15 @@ kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t 
     if (!how->top_p_rows && !(how->top_p > 0.f)) return fail(h, KGQ_E_INVALID_ARG, "top_p must be > 0");
     if (!how->min_p_rows && !(how->min_p >= 0.f && how->min_p <= 1.f))
         return fail(h, KGQ_E_INVALID_ARG, "min_p outside [0, 1]");
+    kgq_status st = check_workspace(h, ws, ws_bytes, sample_workspace(batch, N));
+    if (st != KGQ_OK) return st;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     DeviceGuard dev;
     Lane* L = nullptr;
-    kgq_status st = rows_begin(h, dev, s, &L);
+    st = rows_begin(h, dev, s, &L);
     if (st != KGQ_OK) return st;
     launch_sample({scores, dtype, ld, N, batch, n_draws, how->temperature, how->top_k, how->top_p, how->min_p,
-                   how->temperature_rows, how->top_k_rows, how->top_p_rows, how->min_p_rows, u, out_idx, out_logp,
+                   how->temperature_rows, how->top_k_rows, how->top_p_rows, how->min_p_rows, u, out_idx, out_logp, ws,
                    L ? L->dflag : nullptr},
                   s);
     return rows_end(h, L, s, "");
@@ -1828,21 +1847,17 @@ kgq_status kgq_embed_grad(kgq_handle* h, const void* grad, int32_t dtype, int32_
 {
     if (!h) return KGQ_E_INVALID_ARG;
     if (n < 0) return fail(h, KGQ_E_INVALID_ARG, "n must be >= 0");
-    if (!out || !ws || (n && (!ids || !grad)))
-        return fail(h, KGQ_E_INVALID_ARG, "grad, ids, out and ws must not be NULL");
+    if (!out || (n && (!ids || !grad))) return fail(h, KGQ_E_INVALID_ARG, "grad, ids and out must not be NULL");
     if (!is_dtype(dtype) || !is_dtype(out_dtype)) return fail(h, KGQ_E_INVALID_ARG, "unknown dtype");
     if (rows < 1 || rows > 0x7fffffffLL) return fail(h, KGQ_E_INVALID_ARG, "rows outside [1, 2^31-1]");
     if (dim < 1) return fail(h, KGQ_E_INVALID_ARG, "dim must be >= 1");
     if (ld < dim || ld_out < dim) return fail(h, KGQ_E_INVALID_ARG, "ld and ld_out must be >= dim");
-    if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(h, KGQ_E_INVALID_ARG, "ws must be 16-byte aligned");
-    const int64_t need = embed_grad_workspace(n, dim);
-    if (ws_bytes < (size_t)need)
-        return fail(h, KGQ_E_INVALID_ARG, "ws holds fewer than the " + std::to_string(need) +
-                                              " bytes of kgq_embed_grad_workspace");
+    kgq_status st = check_workspace(h, ws, ws_bytes, embed_grad_workspace(n, dim));
+    if (st != KGQ_OK) return st;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     DeviceGuard dev;
     Lane* L = nullptr;
-    kgq_status st = rows_begin(h, dev, s, &L);
+    st = rows_begin(h, dev, s, &L);
     if (st != KGQ_OK) return st;
     launch_embed_grad({grad, dtype, n, dim, ld, ids, rows, scale, out, out_dtype, ld_out, accumulate, ws,
                        L ? L->dflag : nullptr},

@@ -479,8 +479,6 @@ int64_t topk_scratch_elems(int64_t n_rows, int64_t N, int k);
 // ---- drawing, distillation, embedding rows (k_sample, k_distill, k_rows) ----
 // flag: device error bits, or nullptr (not checked).
 
-constexpr int kSampleThreads = 1024;
-
 struct SampleArgs {
     const void* scores; int dtype; int64_t ld; int64_t N;
     int batch, S;
@@ -488,8 +486,10 @@ struct SampleArgs {
     const float* temperature_rows; const int32_t* top_k_rows; const float* top_p_rows; const float* min_p_rows;
     const float* u;                    // [batch x S]
     int32_t* idx; float* logp;         // [batch x S]; logp or nullptr
+    void* ws;                          // sample_workspace bytes
     int* flag;
 };
+int64_t sample_workspace(int64_t batch, int64_t N);
 void launch_sample(const SampleArgs& a, hipStream_t s);
 
 struct DistillArgs {

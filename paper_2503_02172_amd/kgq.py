@@ -92,7 +92,9 @@ def lib() -> ctypes.CDLL:
         "kgq_memory": ([vp, i64p, i64p], i32),
         "kgq_rank_answers": ([vp, i32, vp, i64, vp, vp, vp, vp, vp, vp], i32),
         "kgq_dense": ([vp, vp, i32, i32, vp, vp, i32, i32, vp, vp], i32),
-        "kgq_sample": ([vp, i32, vp, i32, i64, ctypes.POINTER(Sampling), vp, i32, vp, vp, vp], i32),
+        "kgq_sample": ([vp, i32, vp, i32, i64, ctypes.POINTER(Sampling), vp, i32, vp, vp, vp,
+                        ctypes.c_size_t, vp], i32),
+        "kgq_sample_workspace": ([vp, i32, ctypes.POINTER(ctypes.c_size_t)], i32),
         "kgq_distill": ([vp, i32, vp, i32, i64, i32, vp, vp, ctypes.c_float, vp, vp, vp, i64, vp], i32),
         "kgq_embed": ([vp, vp, i32, i64, i32, i64, vp, i32, ctypes.c_float, vp, i32, i64, vp], i32),
         "kgq_embed_grad_workspace": ([vp, i64, i32, i32, ctypes.POINTER(ctypes.c_size_t)], i32),
@@ -409,12 +411,17 @@ class Engine:
                 kept.append(value)
             else:
                 setattr(how, name, value)
+        need = ctypes.c_size_t()
+        rc = lib().kgq_sample_workspace(self.h, B, ctypes.byref(need))
+        if rc != OK:
+            raise KgqError(rc, "sample: batch outside [1, 2^20]")
         ts = self._rows_stream(stream, kept)
         with torch.cuda.stream(ts):
             idx = torch.empty(u.shape, dtype=torch.int32, device=u.device)
             lp = torch.empty(u.shape, dtype=torch.float32, device=u.device) if logp else None
+            ws = torch.empty(need.value, dtype=torch.uint8, device=u.device)
         self._check(lib().kgq_sample(self.h, B, _ptr(scores), dt, ld, ctypes.byref(how), _ptr(u), u.shape[1],
-                                     _ptr(idx), _ptr(lp), _stream(ts)))
+                                     _ptr(idx), _ptr(lp), _ptr(ws), need.value, _stream(ts)))
         return idx, lp
 
     def distill(self, scores, idx, score, temperature: float = 1.0, weight=None, loss: bool = True,

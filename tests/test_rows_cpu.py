@@ -18,10 +18,11 @@ def eng():
     return kgq.Engine(kgq.GQE, 50, 6, 8, 12.0, 4, device=-1)
 
 
-def sample(e, batch=2, scores=P, dtype=0, ld=50, u=P, S=3, idx=P, logp=None, how=True, **kw):
+def sample(e, batch=2, scores=P, dtype=0, ld=50, u=P, S=3, idx=P, logp=None, how=True, ws=P,
+           ws_bytes=1 << 30, **kw):
     h = kgq.Sampling(**{**OK_HOW, **kw})
     return kgq.lib().kgq_sample(e.h if e else None, batch, scores, dtype, ld, ctypes.byref(h) if how else None, u, S,
-                                idx, logp, None)
+                                idx, logp, ws, ws_bytes, None)
 
 
 def test_sample_refusals(eng):
@@ -32,6 +33,15 @@ def test_sample_refusals(eng):
                 dict(temperature=float("inf")), dict(top_k=-1), dict(top_p=0.0), dict(top_p=-0.5),
                 dict(top_p=float("nan")), dict(min_p=-0.1), dict(min_p=1.5), dict(min_p=float("nan"))):
         assert sample(eng, **bad) == -1, bad
+    need = ctypes.c_size_t()
+    L = kgq.lib()
+    assert L.kgq_sample_workspace(eng.h, 2, ctypes.byref(need)) == 0 and need.value > 0
+    for bad in (dict(ws=None), dict(ws=ctypes.c_void_p(4104)), dict(ws_bytes=need.value - 1)):
+        assert sample(eng, **bad) == -1, bad
+    assert sample(eng, ws_bytes=need.value) == -5
+    for bad in (0, (1 << 20) + 1):
+        assert L.kgq_sample_workspace(eng.h, bad, ctypes.byref(need)) == -1
+    assert L.kgq_sample_workspace(eng.h, 2, None) == -1 and L.kgq_sample_workspace(None, 2, ctypes.byref(need)) == -1
     # a row's own settings take the place of the number, which is not looked at
     assert sample(eng, temperature=-1.0, temperature_rows=4096) == -5
     assert sample(eng, temperature=0.0, top_k=0, top_p=7.0, min_p=1.0) == -5
