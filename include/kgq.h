@@ -493,10 +493,10 @@ kgq_status kgq_dense(kgq_handle* h, const float* x, int32_t M, int32_t K, const 
  *   min_p        of these, keep those of at least this share of the largest
  *                weight, in [0, 1] */
 typedef struct {
-    float temperature;
+    double temperature;
+    double top_p;
+    double min_p;
     int32_t top_k;
-    float top_p;
-    float min_p;
     const float* temperature_rows;
     const int32_t* top_k_rows;
     const float* top_p_rows;
@@ -504,7 +504,7 @@ typedef struct {
 } kgq_sampling;
 
 /* Device bytes of workspace for a kgq_sample of this batch (0 for n_entities
- * above 2^23). Errors: INVALID_ARG (NULL argument, batch outside [1, 2^20]). */
+ * above 327,680). Errors: INVALID_ARG (NULL argument, batch outside [1, 2^20]). */
 kgq_status kgq_sample_workspace(const kgq_handle* h, int32_t batch, size_t* bytes);
 
 /* Draw n_draws entities for each row of scores, with replacement, from given

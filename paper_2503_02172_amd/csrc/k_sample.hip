@@ -38,17 +38,15 @@ namespace {
 
 constexpr int kBins = 2048;
 constexpr int kSort = 2048;                  // entries that are sorted for a cut
+constexpr int kRankSort = 512;               // of these, sorted by counting
+constexpr int kDrawn = 1024;                 // draws of a row whose logarithms are taken together
 constexpr int kRun = 16;                     // lanes per draw, and per 64 scores
 constexpr int kPiece = 1024;                 // scores of a row per wavefront, without cuts
-constexpr int kMaxPieces = 8192;             // of a row (their running sums lie in LDS)
+constexpr int kMaxPieces = 320;              // of a row (their chunks' running sums lie in LDS)
 
-// 2^t for t <= 0 in doubles, 0 below 2^-1074 and for NaN. On |r| <= 1/2 the
-// polynomial interpolates 2^r at Chebyshev's points; it is off by 3e-16.
-__device__ __forceinline__ double pow2d(double t)
+// 2^r on |r| <= 1/2, off by 3e-16: the polynomial through Chebyshev's points.
+__device__ __forceinline__ double pow2_part(double r)
 {
-    t = fmax(t, -1100.0);                    // (a NaN goes here too)
-    const double n = rint(t);
-    const double r = t - n;
     double y = 7.072585949269223e-09;
     y = fma(y, r, 1.0208690299958306e-07);
     y = fma(y, r, 1.321544258792169e-06);
@@ -59,21 +57,53 @@ __device__ __forceinline__ double pow2d(double t)
     y = fma(y, r, 0.05550410866444772);
     y = fma(y, r, 0.24022650695910097);
     y = fma(y, r, 0.69314718055995);
-    y = fma(y, r, 1.0);
-    return ldexp(y, (int)n);
+    return fma(y, r, 1.0);
+}
+// 2^t for t <= 0, 0 below 2^-1074 and for NaN.
+__device__ __forceinline__ double pow2d(double t)
+{
+    t = fmax(t, -1100.0);                    // (a NaN goes here too)
+    const double n = rint(t);
+    return ldexp(pow2_part(t - n), (int)n);
 }
 
-// A row's weights. Where the maximum is +inf, the infinite scores share the
-// weight.
+// A row's weights, 2^((x - M) c) with c = log2(e) / T; 0 below 2^-1000, for
+// -inf and NaN. Where the maximum is +inf, the infinite scores share the
+// weight. Rounding and scaling by n take an addition each instead of the
+// instructions of that name, which run at a quarter of the rate or less: the
+// sum of 1.5 2^52 and a number holds it rounded in its low bits, and adding n to
+// the exponent field multiplies by 2^n. (The sums of 2,048 rows of 63,361: 132
+// us with those instructions.)
 struct RowWeight {
-    float M;
-    double c;                                // log2(e) / T
+    float top, low, from;                    // scores are taken into [low, top]; below `from` they have no weight
+    double M, c;
+    __device__ __forceinline__ RowWeight(float max, double T)
+    {
+        constexpr float kMax = 3.4028234664e38f;
+        const bool inf = max == INFINITY;
+        top = fminf(max, kMax);
+        low = inf ? kMax : fmaxf(max - 693.f * (float)T, -kMax);
+        from = inf ? INFINITY : low;
+        M = top;
+        c = fmin(1.4426950408889634074 / T, 1e300);      // (times 0 for the largest score)
+    }
+    // (for scores of weight; not clamped)
     __device__ __forceinline__ double exponent(float x) const
     {
-        if (M == INFINITY) return x == INFINITY ? 0.0 : -INFINITY;
-        return ((double)x - (double)M) * c;
+        if (from == INFINITY) return x == INFINITY ? 0.0 : -INFINITY;
+        return ((double)x - M) * c;
     }
-    __device__ __forceinline__ double operator()(float x) const { return pow2d(exponent(x)); }
+    __device__ __forceinline__ double operator()(float x) const
+    {
+        constexpr double magic = 6755399441055744.0;
+        const double d = (double)__builtin_amdgcn_fmed3f(x, low, top) - M;
+        const double s = fma(d, c, magic);
+        const double y = pow2_part(fma(d, c, magic - s));
+        const int n = max((int)(uint32_t)__builtin_bit_cast(uint64_t, s), -1021);
+        uint64_t u = __builtin_bit_cast(uint64_t, y);
+        u = ((uint64_t)((uint32_t)(u >> 32) + ((uint32_t)n << 20)) << 32) | (uint32_t)u;
+        return x >= from ? __builtin_bit_cast(double, u) : 0.0;
+    }
 };
 
 __device__ __forceinline__ uint64_t ranking(float x, uint32_t i)
@@ -92,13 +122,17 @@ struct SampleLds {
     static constexpr int waves = THREADS / 64;
     union {
         struct {
-            uint32_t count[kBins];
+            alignas(16) uint32_t count[kBins + 64];   // (the last 64: scores that belong to no bin, by lane)
             unsigned long long mass[kBins];
         } h;
         struct {
-            uint64_t c[kSort];
+            alignas(16) uint64_t c[kSort];
             unsigned long long extra[CHUNKS];
         } s;
+        struct {
+            double share[kDrawn];
+            int32_t idx[kDrawn];
+        } d;
     };
     double chunk[CHUNKS];
     float fbuf[waves];
@@ -175,7 +209,9 @@ __device__ __forceinline__ void find_bin(SampleLds<THREADS, CHUNKS>& L, const Cu
 #pragma unroll
     for (int j = 0; j < per; ++j) {
         if (c[j]) {
-            const bool ok = goal.by_mass ? *mass + (mb + m[j]) >= goal.mass : *count + cb + c[j] >= goal.count;
+            // (the bin in which the sum crosses the goal)
+            const bool ok = goal.by_mass ? *mass + (mb + m[j]) >= goal.mass && (*mass + mb < goal.mass || cb == 0)
+                                         : *count + cb + c[j] >= goal.count && *count + cb < goal.count;
             if (ok && met == kBins) {
                 met = tid * per + j;
                 c_at = cb;
@@ -213,6 +249,33 @@ template <int THREADS, int CHUNKS>
 __device__ __forceinline__ void sort_list(SampleLds<THREADS, CHUNKS>& L, int n)
 {
     const int tid = threadIdx.x;
+    if (n <= kRankSort) {
+        // few: an entry's place is the number of larger ones
+        static_assert(kRankSort <= 2 * THREADS, "two entries a thread at most");
+        if (tid == 0 && (n & 1)) L.s.c[n] = 0ull;
+        __syncthreads();
+        uint64_t mine[2];
+        int place[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = tid + k * THREADS;
+            place[k] = -1;
+            if (i >= n) continue;
+            mine[k] = L.s.c[i];
+            int larger = 0;
+            for (int j = 0; j < n; j += 2) {
+                const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&L.s.c[j]);
+                larger += (o.x > mine[k]) + (o.y > mine[k]);
+            }
+            place[k] = larger;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (place[k] >= 0) L.s.c[place[k]] = mine[k];
+        __syncthreads();
+        return;
+    }
     int P = 2;
     while (P < n) P <<= 1;
     for (int i = n + tid; i < P; i += THREADS) L.s.c[i] = 0ull;
@@ -255,9 +318,11 @@ __device__ __forceinline__ uint32_t sorted_cut(SampleLds<THREADS, CHUNKS>& L, in
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < per; ++j) {
-        before += w[j];
         const int i = tid * per + j;
-        if (i < n && mass + before >= goal.mass) atomicMin(&L.n, (uint32_t)i);
+        const bool short_of = mass + before < goal.mass;
+        before += w[j];
+        // (the entry at which the sum crosses the goal)
+        if (i < n && mass + before >= goal.mass && (short_of || i == 0)) atomicMin(&L.n, (uint32_t)i);
     }
     __syncthreads();
     return L.n;
@@ -279,7 +344,7 @@ __device__ __forceinline__ uint64_t find_cut(SampleLds<THREADS, CHUNKS>& L, cons
     double mass = 0.0;
     unsigned long long lo = floor, hi = ~0ull;
     auto bin_of = [&](float x) {
-        const float v = (wt.M - x) * inv;        // 0 and up; NaN (infinite M, or a step of 0) to bin 0
+        const float v = (wt.top - x) * inv;        // 0 and up; NaN (infinite M, or a step of 0) to bin 0
         return v < (float)(kBins - 1) ? max((int)v, 0) : v >= (float)(kBins - 1) ? kBins - 1 : 0;
     };
     for (int level = 0;; ++level) {
@@ -396,30 +461,32 @@ __device__ __forceinline__ void load4(const T* row, int64_t i, int64_t N, float 
     end4(x, i, N);
 }
 
-// Sum over 16 neighbouring lanes, the same in each.
+// A double from another lane of the 16, by DPP (0 where there is none).
+template <int CTRL>
+__device__ __forceinline__ double dpp16(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xF, 0xF, false);
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+// Sum over 16 neighbouring lanes, the same in each: neighbours, pairs, half
+// rows mirrored, rows mirrored.
 __device__ __forceinline__ double sum16(double x)
 {
-    auto step = [&](auto ctrl) {
-        const uint64_t u = __builtin_bit_cast(uint64_t, x);
-        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, decltype(ctrl)::value, 0xF, 0xF, false);
-        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), decltype(ctrl)::value, 0xF, 0xF, false);
-        x += __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
-    };
-    step(std::integral_constant<int, 0xB1>());       // neighbours
-    step(std::integral_constant<int, 0x4E>());       // pairs
-    step(std::integral_constant<int, 0x141>());      // half rows mirrored
-    step(std::integral_constant<int, 0x140>());      // rows mirrored
+    x += dpp16<0xB1>(x);
+    x += dpp16<0x4E>(x);
+    x += dpp16<0x141>(x);
+    x += dpp16<0x140>(x);
     return x;
 }
-
+// Running sum over 16 lanes (rows shifted by 1, 2, 4 and 8).
 __device__ __forceinline__ double scan16(double x)
 {
-    const int lane = threadIdx.x & (kRun - 1);
-#pragma unroll
-    for (int d = 1; d < kRun; d <<= 1) {
-        const double o = __shfl_up(x, d, kRun);
-        if (lane >= d) x += o;
-    }
+    x += dpp16<0x111>(x);
+    x += dpp16<0x112>(x);
+    x += dpp16<0x114>(x);
+    x += dpp16<0x118>(x);
     return x;
 }
 
@@ -459,17 +526,15 @@ __device__ __forceinline__ int64_t pick16(const T* row, int64_t N, int64_t i0, i
         float x[4];
         double v[4], sum = 0.0;
         load4(row, i, N, x);
+        weigh(x, i, v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = weigh(x[e], i + e);
-            sum += v[e];
-        }
+        for (int e = 0; e < 4; ++e) sum += v[e];
         const double incl = run + scan16(sum);
         const uint32_t some = ballot16(sum > 0.0), over = ballot16(sum > 0.0 && incl > rest);
         // (no lane over yet: the last one with a weight, in case there is no other)
         const int l = over ? __builtin_ctz(over) : some ? 31 - __builtin_clz(some) : -1;
         if (l >= 0) {
-            double before = __shfl_up(incl, 1, kRun);
+            double before = dpp16<0x111>(incl);
             if (lane == 0) before = run;
             int at = 0;
             bool found = false;
@@ -491,25 +556,71 @@ __device__ __forceinline__ int64_t pick16(const T* row, int64_t N, int64_t i0, i
     return pick;
 }
 
+// The same over a row whose chunks of len scores have the running sums run[0 ..
+// n): the first chunk whose sum exceeds the target, and the element in it.
+// Where rounding has the target end in a chunk that holds nothing, the next one
+// that does; behind the total (u = 1), the last one that does.
+template <typename T, typename W>
+__device__ __forceinline__ int64_t pick_in(const T* row, int64_t N, const double* run, int n, int64_t len, double target,
+                                           W weigh, double* w)
+{
+    const int at = search16(run, n, target);
+    bool back = false;
+    for (int c = at;;) {
+        if (c == n) {
+            back = true;
+            c = at - 1;
+        }
+        const double rest = c == at ? target - (c ? run[c - 1] : 0.0) : back ? INFINITY : -1.0;
+        const int64_t i = pick16(row, N, c * len, min(N, (c + 1) * len), rest, weigh, w);
+        if (i >= 0 || (back && c == 0)) return i;
+        c += back ? -1 : 1;
+    }
+}
+
 __device__ __forceinline__ double draw_share(float u) { return u >= 0.f ? fmin((double)u, 1.0) : 0.0; }
+
+// A row's draws, 16 lanes each: draw(target, &weight) returns the entity for a
+// share of the total. Their logarithms are taken afterwards, a lane each.
+template <int THREADS, typename D>
+__device__ __forceinline__ void draw_all(double* share, int32_t* idx, const SampleArgs& a, int64_t b, double total, D draw)
+{
+    const int tid = threadIdx.x;
+    for (int s0 = 0; s0 < a.S; s0 += kDrawn) {
+        const int n = min(kDrawn, a.S - s0);
+        for (int s = tid / kRun; s < n; s += THREADS / kRun) {
+            double w;
+            const int64_t i = draw(draw_share(a.u[b * a.S + s0 + s]) * total, &w);
+            if ((tid & (kRun - 1)) == 0) {
+                share[s] = w;
+                idx[s] = (int32_t)i;
+            }
+        }
+        __syncthreads();
+        for (int s = tid; s < n; s += THREADS) {
+            a.idx[b * a.S + s0 + s] = idx[s];
+            if (a.logp) a.logp[b * a.S + s0 + s] = (float)log(share[s] / total);
+        }
+        __syncthreads();
+    }
+}
 
 // A row's settings.
 struct RowSettings {
-    float temperature, top_p, min_p;
+    double temperature, top_p, min_p;
     int32_t top_k;
     __device__ __forceinline__ RowSettings(const SampleArgs& a, int64_t b)
-        : temperature(a.temperature_rows ? a.temperature_rows[b] : a.temperature),
-          top_p(a.top_p_rows ? a.top_p_rows[b] : a.top_p),
-          min_p(a.min_p_rows ? a.min_p_rows[b] : a.min_p),
+        : temperature(a.temperature_rows ? (double)a.temperature_rows[b] : a.temperature),
+          top_p(a.top_p_rows ? (double)a.top_p_rows[b] : a.top_p),
+          min_p(a.min_p_rows ? (double)a.min_p_rows[b] : a.min_p),
           top_k(a.top_k_rows ? a.top_k_rows[b] : a.top_k)
     {
     }
     __device__ __forceinline__ bool bad() const
     {
-        return !(temperature >= 0.f && temperature < INFINITY) || top_k < 0 || !(top_p > 0.f) ||
-               !(min_p >= 0.f && min_p <= 1.f);
+        return !(temperature >= 0.0 && temperature < INFINITY) || top_k < 0 || !(top_p > 0.0) ||
+               !(min_p >= 0.0 && min_p <= 1.0);
     }
-    __device__ __forceinline__ double c() const { return 1.4426950408889634074 / (double)temperature; }
 };
 
 }  // namespace
@@ -528,26 +639,27 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_sample_sums(SampleArgs a, SamplePieces q)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t b = wave / q.pieces, piece = wave % q.pieces;
-    if (b >= a.batch) return;
+    const int64_t b = blockIdx.x;
+    const int piece = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (piece >= q.pieces) return;
+    const int64_t wave = b * q.pieces + piece;
     const T* row = reinterpret_cast<const T*>(a.scores) + b * a.ld;
     Four<T> f[4];
     float x[4][4], best = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j].load(row, piece * kPiece + j * 256 + lane * 4, a.N);
+    for (int j = 0; j < 4; ++j) f[j].load(row, (int64_t)piece * kPiece + j * 256 + lane * 4, a.N);
 #pragma unroll
     for (int j = 0; j < 4; ++j) f[j].get(x[j]);
-    if ((piece + 1) * kPiece > a.N) {
+    if ((int64_t)(piece + 1) * kPiece > a.N) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) end4(x[j], piece * kPiece + j * 256 + lane * 4, a.N);
+        for (int j = 0; j < 4; ++j) end4(x[j], (int64_t)piece * kPiece + j * 256 + lane * 4, a.N);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) best = fmaxf(best, x[j][e]);
     best = wave_reduce(best, OpMax());
-    const RowWeight wt{best, RowSettings(a, b).c()};
+    const RowWeight wt(best, RowSettings(a, b).temperature);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const double s = sum16((wt(x[j][0]) + wt(x[j][1])) + (wt(x[j][2]) + wt(x[j][3])));
@@ -559,33 +671,37 @@ __global__ __launch_bounds__(256) void k_sample_sums(SampleArgs a, SamplePieces 
 template <typename T>
 __global__ __launch_bounds__(256) void k_sample_draw(SampleArgs a, SamplePieces q)
 {
-    extern __shared__ double run[];                  // [pieces]
-    __shared__ float fbuf[4];
-    __shared__ double dbuf[4];
+    constexpr int DT = 256;
+    extern __shared__ double run[];                  // [16 pieces]: the chunks' running sums
+    __shared__ float fbuf[DT / 64];
+    __shared__ double dbuf[DT / 64];
     __shared__ uint32_t first;
-    const int tid = threadIdx.x, lane = tid & (kRun - 1);
+    __shared__ double share[kDrawn];
+    __shared__ int32_t idx[kDrawn];
+    const int tid = threadIdx.x;
     const int64_t b = blockIdx.x, N = a.N;
     const T* row = reinterpret_cast<const T*>(a.scores) + b * a.ld;
     const float* best = q.best + b * q.pieces;
     const double* sums = q.sums + b * q.pieces * 16;
+    const int n = q.pieces * 16;
     int32_t* out = a.idx + b * a.S;
     float* logp = a.logp ? a.logp + b * a.S : nullptr;
     const RowSettings set(a, b);
     if (set.bad() && a.flag && tid == 0) atomicOr(a.flag, kErrSettings);
     float M = -INFINITY;
-    for (int i = tid; i < q.pieces; i += 256) M = fmaxf(M, best[i]);
-    M = block_reduce<4>(M, fbuf, OpMax());
+    for (int i = tid; i < q.pieces; i += DT) M = fmaxf(M, best[i]);
+    M = block_reduce<DT / 64>(M, fbuf, OpMax());
     if (set.bad() || M == -INFINITY) {               // nothing to draw from
-        for (int s = tid; s < a.S; s += 256) {
+        for (int s = tid; s < a.S; s += DT) {
             out[s] = -1;
             if (logp) logp[s] = __builtin_nanf("");
         }
         return;
     }
-    if (set.temperature == 0.f) {                    // the first of the best
+    if (set.temperature == 0.0) {                    // the first of the best
         if (tid == 0) first = ~0u;
         __syncthreads();
-        for (int i = tid; i < q.pieces; i += 256)
+        for (int i = tid; i < q.pieces; i += DT)
             if (best[i] == M) {
                 atomicMin(&first, (uint32_t)i);
                 break;
@@ -595,63 +711,43 @@ __global__ __launch_bounds__(256) void k_sample_draw(SampleArgs a, SamplePieces 
         __syncthreads();
         if (tid == 0) first = ~0u;
         __syncthreads();
-        for (int64_t i = i0 + tid; i < min(N, i0 + kPiece); i += 256)
+        for (int64_t i = i0 + tid; i < min(N, i0 + kPiece); i += DT)
             if (row_value(row[i]) == M) {
                 atomicMin(&first, (uint32_t)i);
                 break;
             }
         __syncthreads();
-        for (int s = tid; s < a.S; s += 256) {
+        for (int s = tid; s < a.S; s += DT) {
             out[s] = (int32_t)first;
             if (logp) logp[s] = 0.f;
         }
         return;
     }
-    const RowWeight wt{M, set.c()};
-    // running sums over the pieces: a thread's share of them, then the threads'
-    const int per = (q.pieces + 255) / 256;
+    const RowWeight wt(M, set.temperature);
+    for (int i = tid; i < n; i += DT) run[i] = sums[i] * wt(best[i >> 4]);
+    __syncthreads();
+    const int per = (n + DT - 1) / DT;
     double sum = 0.0, total;
     for (int j = 0; j < per; ++j) {
         const int i = tid * per + j;
-        if (i < q.pieces) {
-            double s = 0.0;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s += sums[(int64_t)i * 16 + e];
-            sum += s * wt(best[i]);
+        if (i < n) {
+            sum += run[i];
             run[i] = sum;
         }
     }
-    const double before = block_scan<4>(sum, dbuf, &total) - sum;
+    const double before = block_scan<DT / 64>(sum, dbuf, &total) - sum;
     for (int j = 0; j < per; ++j)
-        if (tid * per + j < q.pieces) run[tid * per + j] += before;
+        if (tid * per + j < n) run[tid * per + j] += before;
     __syncthreads();
-    total = run[q.pieces - 1];
-    for (int s = tid / kRun; s < a.S; s += 256 / kRun) {
-        const double target = draw_share(a.u[b * a.S + s]) * total;
-        int piece = search16(run, q.pieces, target);
-        if (piece == q.pieces) {                     // (u = 1) the last one that holds something
-            piece = q.pieces - 1;
-            while (piece > 0 && run[piece - 1] == total) --piece;
-        }
-        const float top = best[piece];
-        const double scale = wt(top);
-        double rest = (target - (piece ? run[piece - 1] : 0.0)) / scale;
-        // its chunks
-        const double mine = sums[(int64_t)piece * 16 + lane];
-        const double incl = scan16(mine);
-        const uint32_t some = ballot16(mine > 0.0), over = ballot16(mine > 0.0 && incl > rest);
-        const int c = over ? __builtin_ctz(over) : 31 - __builtin_clz(some | 1u);
-        const double ahead = __shfl(incl - mine, c, kRun);
-        rest -= ahead;
-        const int64_t i0 = (int64_t)piece * kPiece + c * 64;
-        const RowWeight in_piece{top, wt.c};
-        double w;
-        const int64_t i = pick16(row, N, i0, i0 + 64, rest, [&](float x, int64_t) { return in_piece(x); }, &w);
-        if (lane == 0) {
-            out[s] = (int32_t)i;
-            if (logp) logp[s] = (float)log(w * scale / total);
-        }
-    }
+    total = run[n - 1];
+    draw_all<DT>(share, idx, a, b, total, [&](double target, double* w) {
+        return pick_in(row, N, run, n, 64, target,
+                      [&](const float (&x)[4], int64_t, double (&v)[4]) {
+#pragma unroll
+                          for (int e = 0; e < 4; ++e) v[e] = wt(x[e]);
+                      },
+                      w);
+    });
 }
 
 // ---- with cuts ------------------------------------------------------------------
@@ -659,6 +755,15 @@ __global__ __launch_bounds__(256) void k_sample_draw(SampleArgs a, SamplePieces 
 namespace {
 
 constexpr int kPending = -2;                 // in a row's first index: k_sample_rows left the row to k_sample_far
+
+// Scores per running sum, as a power of two: 64 or as many as CHUNKS sums need.
+template <int CHUNKS>
+__device__ __forceinline__ int chunk_shift(int64_t N)
+{
+    int shift = 6;
+    while (((N + (1ll << shift) - 1) >> shift) > CHUNKS) ++shift;
+    return shift;
+}
 
 // A row with nothing to draw from.
 template <int THREADS>
@@ -695,26 +800,17 @@ __device__ __forceinline__ void draw_kept(SampleLds<THREADS, CHUNKS>& L, const S
     }
     __syncthreads();
     total = L.chunk[n_chunks - 1];
-    for (int s = tid / kRun; s < a.S; s += THREADS / kRun) {
-        const double target = draw_share(a.u[b * a.S + s]) * total;
-        int c = search16(L.chunk, n_chunks, target);
-        if (c == n_chunks) {                         // (u = 1) the last one that holds something
-            c = n_chunks - 1;
-            while (c > 0 && L.chunk[c - 1] == total) --c;
-        }
-        double w;
-        const int64_t i = pick16(row, N, c * len, min(N, (c + 1) * len), target - (c ? L.chunk[c - 1] : 0.0),
-                                 [&](float x, int64_t at) {
-                                     if (!(x > -INFINITY) || ranking(x, (uint32_t)at) < cut) return 0.0;
-                                     const double v = wt(x);
-                                     return v >= min_p ? v : 0.0;
-                                 },
-                                 &w);
-        if ((tid & (kRun - 1)) == 0) {
-            a.idx[b * a.S + s] = (int32_t)i;
-            if (a.logp) a.logp[b * a.S + s] = (float)log(w / total);
-        }
-    }
+    draw_all<THREADS>(L.d.share, L.d.idx, a, b, total, [&](double target, double* w) {
+        return pick_in(row, N, L.chunk, n_chunks, len, target,
+                      [&](const float (&x)[4], int64_t at, double (&v)[4]) {
+#pragma unroll
+                          for (int e = 0; e < 4; ++e) {
+                              v[e] = wt(x[e]);
+                              if (ranking(x[e], (uint32_t)(at + e)) < cut || !(v[e] >= min_p)) v[e] = 0.0;
+                          }
+                      },
+                      w);
+    });
 }
 
 }  // namespace
@@ -763,7 +859,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
         }
     }
     // f(first element, four scores), the same number of times in every thread
-    auto each = [&](auto f) {
+    auto each = [&](auto f) __attribute__((always_inline)) {
         if constexpr (NV > 0) {
 #pragma unroll 1
             for (int j = 0; j < NV; ++j) {
@@ -798,7 +894,10 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
         draw_nothing<THREADS>(a, b);
         return;
     }
-    if (set.temperature == 0.f || set.top_k == 1) {  // the first in ranking order
+    auto leave = [&]() __attribute__((always_inline)) {
+        if (tid == 0) a.idx[b * a.S] = kPending;
+    };
+    if (set.temperature == 0.0 || set.top_k == 1) {  // the first in ranking order
         if (tid == 0) L.n = ~0u;
         __syncthreads();
         uint32_t first = ~0u;
@@ -815,32 +914,41 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
         }
         return;
     }
-    const RowWeight wt{M, set.c()};
-    const double min_p = (double)set.min_p;
+    if (M == INFINITY) return leave();
+    const RowWeight wt(M, set.temperature);
+    const double min_p = set.min_p;
     uint64_t cut = 0;                                // what is kept: composites from here on
 
     // Histogram of the distances from M over `range`, of what is kept so far.
+    // Scores further off are in no bin, masked ones neither (their place in a
+    // counter of the lane's own keeps the lanes together).
     float inv = 0.f, step = 0.f;
-    auto bin_of = [&](float x) {
-        const float v = (M - x) * inv;
-        return v < (float)(kBins - 1) ? (int)v : kBins - 1;
-    };
-    auto histogram = [&](float range) {
-        step = range / (float)(kBins - 1);
+    auto bin_of = [&](float x) __attribute__((always_inline)) { return (M - x) * inv; };   // rounded down, below kBins
+    auto histogram = [&](float range) __attribute__((always_inline)) {
+        step = range / (float)kBins;
         inv = 1.0f / step;
         for (int i = tid; i < kBins; i += THREADS) L.h.count[i] = 0;
         __syncthreads();
         each([&](int64_t i, const float (&x)[4]) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (x[e] > -INFINITY && (!cut || ranking(x[e], (uint32_t)(i + e)) >= cut))
-                    atomicAdd(&L.h.count[bin_of(x[e])], 1u);
+            for (int e = 0; e < 4; ++e) {
+                const float v = bin_of(x[e]);
+                int bin = v < (float)kBins ? (int)v : kBins + (tid & 63);
+                if (cut) bin = ranking(x[e], (uint32_t)(i + e)) >= cut ? bin : kBins + (tid & 63);
+                atomicAdd(&L.h.count[bin], 1u);
+            }
         });
         __syncthreads();
     };
     constexpr float kNormal = 1.1754944e-38f * kBins;   // ranges whose steps have an inverse
-    auto leave = [&]() {
-        if (tid == 0) a.idx[b * a.S] = kPending;
+    auto lowest = [&]() __attribute__((always_inline)) {
+        float low = M;
+        each([&](int64_t, const float (&x)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) low = fminf(low, x[e] > -INFINITY ? x[e] : M);
+        });
+        __syncthreads();
+        return -block_reduce<SW>(-low, L.fbuf, OpMax());
     };
 
     if (set.top_k > 0 && set.top_k < N) {
@@ -851,16 +959,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
             __syncthreads();
             low = -block_reduce<SW>(-mine, L.fbuf, OpMax());
         }
-        if (low == -INFINITY) {
-            low = M;
-            each([&](int64_t, const float (&x)[4]) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (x[e] > -INFINITY) low = fminf(low, x[e]);
-            });
-            __syncthreads();
-            low = -block_reduce<SW>(-low, L.fbuf, OpMax());
-        }
+        if (low == -INFINITY) low = lowest();
         const CutGoal goal{false, (uint32_t)set.top_k, 0.0};
         const float range = (M - low) * 1.0001f;
         if (!(range > kNormal && range < INFINITY)) return leave();
@@ -876,7 +975,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
         each([&](int64_t i, const float (&x)[4]) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (x[e] > -INFINITY && bin_of(x[e]) == bin)
+                if (bin_of(x[e]) >= (float)bin && bin_of(x[e]) < (float)(bin + 1))
                     L.s.c[atomicAdd(&L.n, 1u)] = ranking(x[e], (uint32_t)(i + e));
         });
         __syncthreads();
@@ -886,12 +985,14 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
     }
 
     // the bins that top-p's cut lies in, by the counts
-    const bool by_mass = set.top_p < 1.f;
-    int from = kBins, to = kBins;
+    const double p = set.top_p;
+    const bool by_mass = p < 1.0;
+    float from = INFINITY, to = INFINITY;            // their distances: from this one, below that one
     if (by_mass) {
-        // entries further off than this hold less than a 1,000th of 1 - p together
-        const float range = (logf((float)N) - logf(1.f - set.top_p) + 8.f) * set.temperature;
-        if (!(M < INFINITY && range > kNormal && range < INFINITY)) return leave();
+        // entries further off than this hold less than e^-8 of 1 - p together
+        const float far = (logf((float)N) - logf((float)(1.0 - set.top_p)) + 8.f) * (float)set.temperature;
+        const float range = fminf(far, (M - lowest()) * 1.0001f);
+        if (!(range > kNormal && range < INFINITY)) return leave();
         histogram(range);
         constexpr int per = kBins / THREADS;
         double m[per], sum = 0.0, all;
@@ -903,7 +1004,9 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
             sum += m[j];
         }
         double run = block_scan<SW>(sum, L.dbuf, &all) - sum;
-        const double margin = fmin(1e-3, 0.5 - 0.5 * (double)set.top_p);
+        // A bin's sum is off by up to half a step's weight, h, a share f of the
+        // whole thus by 2 h f (1 - f); the entries behind the range add e^-8 f (1 - f).
+        const double margin = (0.75 * (double)step * wt.c + 5e-4) * p * (1.0 - p) + 1e-9;
         if (tid == 0) {
             L.bin = kBins;
             L.last = kBins;
@@ -912,43 +1015,60 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < per; ++j) {
+            const double lo = (p - margin) * all, hi = fmin(p + margin, 1.0 - 1e-12) * all;
+            const double before = run;
             run += m[j];
-            if (c[j] && run >= ((double)set.top_p - margin) * all) atomicMin(&L.bin, tid * per + j);
-            if (c[j] && run >= ((double)set.top_p + margin) * all) atomicMin(&L.last, tid * per + j);
+            // (where the sum crosses the border: a bin or two)
+            if (run >= lo && (before < lo || tid + j == 0)) atomicMin(&L.bin, tid * per + j);
+            if (run >= hi && before < hi) atomicMin(&L.last, tid * per + j);
         }
         for (int i = tid; i < CHUNKS; i += THREADS) L.s.extra[i] = 0ull;
         __syncthreads();
-        from = L.bin;
-        to = L.last;
+        if (L.bin == kBins || L.last == kBins) return leave();
+        from = (float)L.bin;
+        to = (float)(L.last + 1);
     }
 
     // One pass in doubles: sums in index order, the total, and for top-p what
     // lies before the bins and the list of what lies in them.
-    int64_t len = 64;
-    while ((N + len - 1) / len > CHUNKS) len <<= 1;
-    const int n_chunks = (int)((N + len - 1) / len);
+    const int shift = chunk_shift<CHUNKS>(N);
+    const int64_t len = 1ll << shift;
+    const int n_chunks = (int)((N + len - 1) >> shift);
     double z = 0.0, above = 0.0;
-    auto four = [&](int64_t i, const float (&x)[4]) {
-        double sum = 0.0;
+    auto four = [&](int64_t i, const float (&x)[4]) __attribute__((always_inline)) {
+        double w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            double w = x[e] > -INFINITY ? wt(x[e]) : 0.0;
-            if (cut) w = ranking(x[e], (uint32_t)(i + e)) >= cut ? w : 0.0;
-            const double keep = w >= min_p ? w : 0.0;
-            if (by_mass) {
-                const int bin = bin_of(x[e]);
-                z += w;
-                above += bin < from ? w : 0.0;
-                sum += bin < from ? keep : 0.0;
-                if (bin >= from && bin <= to && w > 0.0) {
-                    const uint32_t at = atomicAdd(&L.n, 1u);
-                    if (at < (uint32_t)kSort) L.s.c[at] = ranking(x[e], (uint32_t)(i + e));
-                }
-            } else {
-                sum += keep;
-            }
+        for (int e = 0; e < 4; ++e) w[e] = wt(x[e]);
+        if (cut) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = ranking(x[e], (uint32_t)(i + e)) >= cut ? w[e] : 0.0;
         }
-        return sum;
+        if (by_mass) {
+            z += (w[0] + w[1]) + (w[2] + w[3]);
+            float v[4];
+            bool in[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = bin_of(x[e]);
+                in[e] = (v[e] >= from) & (v[e] < to);
+            }
+            if (in[0] | in[1] | in[2] | in[3]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (in[e] && w[e] > 0.0) {
+                        const uint32_t at = atomicAdd(&L.n, 1u);
+                        if (at < (uint32_t)kSort) L.s.c[at] = ranking(x[e], (uint32_t)(i + e));
+                    }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = v[e] < from ? w[e] : 0.0;
+        }
+        const double sum = (w[0] + w[1]) + (w[2] + w[3]);
+        above += sum;
+        if (!(min_p > 0.0)) return sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = w[e] >= min_p ? w[e] : 0.0;
+        return (w[0] + w[1]) + (w[2] + w[3]);
     };
     if (NV > 0 || len == 64) {
         each([&](int64_t i, const float (&x)[4]) {
@@ -970,7 +1090,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
     if (by_mass) {
         z = block_reduce<SW>(z, L.dbuf, OpSum());
         above = block_reduce<SW>(above, L.dbuf2, OpSum());
-        const CutGoal goal{true, 0u, (double)set.top_p * z};
+        const CutGoal goal{true, 0u, p * z};
         const uint32_t n = L.n;
         __syncthreads();
         if (n == 0 || n > (uint32_t)kSort || !(above < goal.mass)) return leave();
@@ -983,7 +1103,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
         for (int i = tid; i <= (int)at; i += THREADS) {
             const uint64_t c = L.s.c[i];
             const double w = wt(ranking_score(c));
-            if (w >= min_p) atomicAdd(&L.s.extra[(uint32_t)~c / len], (unsigned long long)(w * unit));
+            if (w >= min_p) atomicAdd(&L.s.extra[(uint32_t)~c >> shift], (unsigned long long)(w * unit));
         }
         __syncthreads();
         for (int i = tid; i < n_chunks; i += THREADS)
@@ -1015,13 +1135,13 @@ __global__ __launch_bounds__(1024) void k_sample_far(SampleArgs a)
     __syncthreads();
     low = -block_reduce<SW>(-low, L.fbuf, OpMax());
     __syncthreads();
-    const RowWeight wt{M, set.c()};
+    const RowWeight wt(M, set.temperature);
     uint64_t cut = 0;
     // (both cuts in one loop: the search is long code)
     for (int turn = 0; turn < 2; ++turn) {
         CutGoal goal{turn == 1, (uint32_t)set.top_k, 0.0};
         float range = M - low;
-        if (turn == 0 ? !(set.top_k > 0 && set.top_k < N) : !(set.top_p < 1.f)) continue;
+        if (turn == 0 ? !(set.top_k > 0 && set.top_k < N) : !(set.top_p < 1.0)) continue;
         if (turn == 1) {
             // the weight that p is a share of
             double sum = 0.0;
@@ -1031,15 +1151,15 @@ __global__ __launch_bounds__(1024) void k_sample_far(SampleArgs a)
             }
             sum = block_reduce<SW>(sum, L.dbuf, OpSum());
             __syncthreads();
-            goal.mass = (double)set.top_p * sum;
+            goal.mass = set.top_p * sum;
             // entries with less than (1 - p) / N of the largest weight lie behind the cut
-            range = fminf((logf((float)N) - logf(1.f - set.top_p) + 1.f) * set.temperature, 1e38f);
+            range = fminf((logf((float)N) - logf((float)(1.0 - set.top_p)) + 1.f) * (float)set.temperature, 1e38f);
         }
         cut = max(cut, find_cut(L, row, N, wt, goal, cut, range));
     }
-    int64_t len = 64;
-    while ((N + len - 1) / len > CHUNKS) len <<= 1;
-    const int n_chunks = (int)((N + len - 1) / len);
+    const int shift = chunk_shift<CHUNKS>(N);
+    const int64_t len = 1ll << shift;
+    const int n_chunks = (int)((N + len - 1) >> shift);
     __syncthreads();
     for (int c = tid / 64; c < n_chunks; c += SW) {
         double sum = 0.0;
@@ -1047,12 +1167,12 @@ __global__ __launch_bounds__(1024) void k_sample_far(SampleArgs a)
         for (int64_t i = c * len + (tid & 63); i < end; i += 64) {
             const float x = row_value(row[i]);
             const double w = x > -INFINITY && ranking(x, (uint32_t)i) >= cut ? wt(x) : 0.0;
-            sum += w >= (double)set.min_p ? w : 0.0;
+            sum += w >= set.min_p ? w : 0.0;
         }
         sum = wave_reduce(sum, OpSum());
         if ((tid & 63) == 0) L.chunk[c] = sum;
     }
-    draw_kept(L, a, b, row, wt, cut, (double)set.min_p, n_chunks, len);
+    draw_kept(L, a, b, row, wt, cut, set.min_p, n_chunks, len);
 }
 
 namespace {
@@ -1062,14 +1182,14 @@ int64_t pieces_of(int64_t N) { return (N + kPiece - 1) / kPiece; }
 template <typename T>
 void launch(const SampleArgs& a, hipStream_t s)
 {
-    const bool cuts = a.top_k_rows || a.top_p_rows || a.min_p_rows || (a.top_k > 0 && a.top_k < a.N) || a.top_p < 1.f ||
-                      a.min_p > 0.f;
+    const bool cuts = a.top_k_rows || a.top_p_rows || a.min_p_rows || (a.top_k > 0 && a.top_k < a.N) || a.top_p < 1.0 ||
+                      a.min_p > 0.0;
     if (!cuts && pieces_of(a.N) <= kMaxPieces) {
         const int pieces = (int)pieces_of(a.N);
         double* sums = reinterpret_cast<double*>(a.ws);
         const SamplePieces q{sums, reinterpret_cast<float*>(sums + (int64_t)a.batch * pieces * 16), pieces};
-        hipLaunchKernelGGL(k_sample_sums<T>, dim3((uint32_t)(((int64_t)a.batch * pieces + 3) / 4)), dim3(256), 0, s, a, q);
-        hipLaunchKernelGGL(k_sample_draw<T>, dim3(a.batch), dim3(256), pieces * sizeof(double), s, a, q);
+        hipLaunchKernelGGL(k_sample_sums<T>, dim3(a.batch, (pieces + 3) / 4), dim3(256), 0, s, a, q);
+        hipLaunchKernelGGL(k_sample_draw<T>, dim3(a.batch), dim3(256), pieces * 16 * sizeof(double), s, a, q);
         return;
     }
     // the row in registers where it fits; short rows four or more to a compute
@@ -1080,7 +1200,7 @@ void launch(const SampleArgs& a, hipStream_t s)
     };
     if (a.N <= 4096) go(k_sample_rows<T, 256, 4, 64>, 256);
     else if (a.N <= 16384) go(k_sample_rows<T, 1024, 4, 256>, 1024);
-    else if (a.N <= 65536) go(k_sample_rows<T, 1024, 16, 1024>, 1024);
+    else if (a.N <= 65536) go(k_sample_rows<T, 512, 32, 1024>, 512);
     else go(k_sample_rows<T, 1024, 0, 4096>, 1024);
 }
 

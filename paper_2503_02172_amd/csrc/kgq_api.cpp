@@ -1765,11 +1765,11 @@ kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t 
     if (n_draws < 1) return fail(h, KGQ_E_INVALID_ARG, "n_draws must be >= 1");
     const int64_t N = h->cfg.n_entities;
     if (ld < N) return fail(h, KGQ_E_INVALID_ARG, "ld must be >= n_entities");
-    if (!how->temperature_rows && !(how->temperature >= 0.f && how->temperature <= 3.4028234e38f))
+    if (!how->temperature_rows && !(how->temperature >= 0.0 && how->temperature <= 1.7e308))
         return fail(h, KGQ_E_INVALID_ARG, "temperature must be finite and >= 0");
     if (!how->top_k_rows && how->top_k < 0) return fail(h, KGQ_E_INVALID_ARG, "top_k must be >= 0");
-    if (!how->top_p_rows && !(how->top_p > 0.f)) return fail(h, KGQ_E_INVALID_ARG, "top_p must be > 0");
-    if (!how->min_p_rows && !(how->min_p >= 0.f && how->min_p <= 1.f))
+    if (!how->top_p_rows && !(how->top_p > 0.0)) return fail(h, KGQ_E_INVALID_ARG, "top_p must be > 0");
+    if (!how->min_p_rows && !(how->min_p >= 0.0 && how->min_p <= 1.0))
         return fail(h, KGQ_E_INVALID_ARG, "min_p outside [0, 1]");
     kgq_status st = check_workspace(h, ws, ws_bytes, sample_workspace(batch, N));
     if (st != KGQ_OK) return st;

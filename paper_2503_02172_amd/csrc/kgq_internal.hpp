@@ -482,7 +482,7 @@ int64_t topk_scratch_elems(int64_t n_rows, int64_t N, int k);
 struct SampleArgs {
     const void* scores; int dtype; int64_t ld; int64_t N;
     int batch, S;
-    float temperature; int32_t top_k; float top_p, min_p;        // every row's, where the arrays below are nullptr
+    double temperature; int32_t top_k; double top_p, min_p;      // every row's, where the arrays below are nullptr
     const float* temperature_rows; const int32_t* top_k_rows; const float* top_p_rows; const float* min_p_rows;
     const float* u;                    // [batch x S]
     int32_t* idx; float* logp;         // [batch x S]; logp or nullptr

@@ -53,8 +53,8 @@ class Config(ctypes.Structure):
 
 
 class Sampling(ctypes.Structure):
-    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
-                ("min_p", ctypes.c_float), ("temperature_rows", ctypes.c_void_p), ("top_k_rows", ctypes.c_void_p),
+    _fields_ = [("temperature", ctypes.c_double), ("top_p", ctypes.c_double), ("min_p", ctypes.c_double),
+                ("top_k", ctypes.c_int32), ("temperature_rows", ctypes.c_void_p), ("top_k_rows", ctypes.c_void_p),
                 ("top_p_rows", ctypes.c_void_p), ("min_p_rows", ctypes.c_void_p)]
 
 
@@ -402,7 +402,7 @@ class Engine:
         if u.dim() != 2:
             raise ValueError("sample: u must be [B x S]")
         self._array("sample", "u", u, torch.float32, (B, u.shape[1]))
-        how = Sampling(1.0, 0, 1.0, 0.0)
+        how = Sampling(1.0, 1.0, 0.0, 0)
         kept = [scores, u]
         for name, value in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
             if torch.is_tensor(value):

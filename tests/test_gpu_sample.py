@@ -10,8 +10,6 @@ from tests import rows_ref as R
 
 pytestmark = pytest.mark.gpu
 
-F = lambda v: float(np.float32(v))
-
 
 def engine(N, **kw):
     return kgq.Engine(kgq.GQE, N, 1, 4, 24.0, 1, **kw)
@@ -47,8 +45,8 @@ def run(eng, x, u, dtype="f32", pad=0, **kw):
 def check(eng, x, u, what, T=1.0, k=0, p=1.0, m=0.0, **kw):
     idx, logp, x = run(eng, x, u, temperature=T, top_k=k, top_p=p, min_p=m, **kw)
     for b in range(x.shape[0]):
-        of = lambda v: v[b] if isinstance(v, np.ndarray) else v
-        R.check_draws(idx[b], logp[b], x[b], u[b], f"{what} row {b}", T=F(of(T)), k=int(of(k)), p=F(of(p)), m=F(of(m)))
+        of = lambda v: float(v[b]) if isinstance(v, np.ndarray) else v
+        R.check_draws(idx[b], logp[b], x[b], u[b], f"{what} row {b}", T=of(T), k=int(of(k)), p=of(p), m=of(m))
 
 
 SETTINGS = [dict(), dict(T=0.0), dict(T=0.3), dict(T=40.0), dict(k=1), dict(k=2), dict(k=50), dict(k=1500),
@@ -192,7 +190,7 @@ def test_gpu_sample_row_offsets_past_32_bits():
     idx, logp = eng.sample(t, torch.as_tensor(u, device="cuda"), top_p=0.9)
     idx, logp = idx.cpu().numpy(), logp.cpu().numpy()
     for b in range(3):
-        R.check_draws(idx[b], logp[b], x[b], u[b], f"row {b}", p=F(0.9))
+        R.check_draws(idx[b], logp[b], x[b], u[b], f"row {b}", p=0.9)
 
 
 def test_gpu_sample_on_another_stream():
