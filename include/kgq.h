@@ -547,7 +547,7 @@ kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t 
  *                  out (shorter lists), as are ids out of range (OUT_OF_RANGE in
  *                  checked mode) and scores of -inf. An entity that occurs more
  *                  than once has the sum of its p
- *   temperature    finite, > 0
+ *   temperature    in [1e-30, 1e30]
  *   row_weight     device float [batch], or NULL (1 for every row)
  *   out_loss       device float [batch] or NULL (without row_weight)
  *   out_grad       device [batch x n_entities] of dtype, row stride ld_grad, or
@@ -563,7 +563,7 @@ kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t 
  * outside [1, 2^20], a stride below n_entities, k or temperature out of range;
  * checked mode under capture), OUT_OF_RANGE (checked), NO_DEVICE, DEVICE. */
 kgq_status kgq_distill(kgq_handle* h, int32_t batch, const void* scores, int32_t dtype, int64_t ld, int32_t k,
-                       const int32_t* teacher_idx, const float* teacher_score, float temperature,
+                       const int32_t* teacher_idx, const float* teacher_score, double temperature,
                        const float* row_weight, float* out_loss, void* out_grad, int64_t ld_grad, void* stream);
 
 /* Rows of a table by id: out[t] = scale * table[ids[t]], t = 0 .. n - 1.

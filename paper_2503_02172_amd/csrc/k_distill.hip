@@ -5,7 +5,9 @@
 //   loss   = tau^2 sum_j p_j (log p_j - log q_{a_j})
 //   grad_i = w tau (q_i - sum_{j: a_j = i} p_j)
 // with w the row's weight. The list's share of the gradient touches k entries,
-// so the row is one softmax: a maximum, a sum, and one product per entry.
+// so the row is one softmax: a maximum, a sum, and one product per entry. One
+// workgroup takes a row; up to 65,536 scores stay in registers from the load to
+// the store, so that the row is read once and written once.
 #include <algorithm>
 
 #include "row_ops.hpp"
@@ -14,9 +16,7 @@ namespace kgq {
 
 namespace {
 
-constexpr int DT = 1024;               // threads per row
-constexpr int DW = DT / 64;
-constexpr int kHash = 2 * kMaxK;       // slots of the list's entities
+constexpr int kHash = 2 * kMaxK;       // slots of the list's entities at most
 
 // exp(d / tau) for d <= 0 by its power of two: d log2(e) / tau = n + r, both
 // of it from d itself, so that the error is the one of exp2 and of d's
@@ -29,122 +29,263 @@ __device__ __forceinline__ float exp_of(float d, float chi, float clo)
     return ldexpf(__builtin_amdgcn_exp2f(r), (int)n);
 }
 
+template <int DW>
 struct DistillLds {
     int32_t key[kHash];
     unsigned long long sum[kHash];
-    float fbuf[DW];
-    double dbuf[DW];
-    double dbuf2[DW];
+    float fbuf[DW], fbuf2[DW];
+    double dbuf[DW], dbuf2[DW], dbuf3[DW];
     int any;
+};
+
+// V elements at p.
+template <typename T, int V>
+struct Elements {
+    typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 };
 
 }  // namespace
 
-// One workgroup per row.
-template <typename T>
-__global__ __launch_bounds__(DT) void k_distill(DistillArgs a, float chi, float clo)
+// One workgroup per row. NV > 0: the row's scores in registers, NV vectors of
+// 16 bytes a thread and one more for the row's end; NV = 0: the row is read
+// twice.
+template <typename T, int DT, int NV>
+__global__ __launch_bounds__(DT) void k_distill(DistillArgs a, float chi, float clo, int slots)
 {
-    __shared__ DistillLds L;
+    constexpr int V = RowVec<T>::n, DW = DT / 64, PER = kMaxK / DT;
+    typedef typename Elements<T, V>::vec vec;
+    __shared__ DistillLds<DW> L;
     const int tid = threadIdx.x;
-    const int64_t b = blockIdx.x;
+    const int64_t b = blockIdx.x, N = a.N;
     const T* z = reinterpret_cast<const T*>(a.scores) + b * a.ld;
     T* g = a.grad ? reinterpret_cast<T*>(a.grad) + b * a.ld_grad : nullptr;
 
-    for (int i = tid; i < kHash; i += DT) {
+    // the teacher's list, PER entries a thread at most
+    int32_t id[PER];
+    float t[PER], zj[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int j = k * DT + tid;
+        id[k] = j < a.k ? a.idx[b * a.k + j] : -1;
+        t[k] = j < a.k ? a.teacher[b * a.k + j] : -INFINITY;
+    }
+    // the row: whole vectors (those past the end load the last whole one and
+    // count as -inf), and the last elements, one by one, in one thread
+    const int64_t whole = N / V;
+    const bool last = tid == (int)(whole % DT);
+    vec raw[NV > 0 ? NV : 1];
+    float x[NV > 0 ? NV : 1][V], tail[V];
+    if constexpr (NV > 0) {
+        if (whole > 0) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                raw[j] = *reinterpret_cast<const vec*>(z + min((int64_t)(j * DT + tid), whole - 1) * V);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) tail[e] = last && whole * V + e < N ? row_value(z[whole * V + e]) : -INFINITY;
+
+    for (int i = tid; i < slots; i += DT) {
         L.key[i] = -1;
         L.sum[i] = 0ull;
     }
     if (tid == 0) L.any = 0;
     __syncthreads();
-
-    // the teacher's list, one entry per thread
-    const double inv_tau = 1.0 / (double)a.tau;
-    int32_t id = -1;
-    float t = -INFINITY, zj = 0.f;
-    if (tid < a.k) {
-        id = a.idx[b * a.k + tid];
-        t = a.teacher[b * a.k + tid];
-        if (id >= a.N || id < -1) {
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        if (id[k] >= N || id[k] < -1) {
             if (a.flag) atomicOr(a.flag, kErrRange);
-            id = -1;
+            id[k] = -1;
         }
-        if (id >= 0) {
-            zj = row_value(z[id]);
-            if (!(t == -INFINITY)) L.any = 1;          // (a NaN is a target: it makes the row NaN)
+        zj[k] = 0.f;
+        if (id[k] >= 0) {
+            zj[k] = row_value(z[id[k]]);
+            if (!(t[k] == -INFINITY)) L.any = 1;       // (a NaN is a target: it makes the row NaN)
         } else {
-            t = -INFINITY;
+            t[k] = -INFINITY;
         }
+        tmax = fmaxf(tmax, t[k]);
     }
-    const float tmax = block_reduce<DW>(t, L.fbuf, OpMax());
+    tmax = block_reduce<DW>(tmax, L.fbuf, OpMax());
     const bool empty = L.any == 0;
-    double e = 0.0;
-    if (id >= 0) e = tmax == INFINITY ? (t == INFINITY ? 1.0 : t != t ? (double)t : 0.0) : exp(((double)t - (double)tmax) * inv_tau);
-    if (t == -INFINITY) e = 0.0;
-    const double zt = block_reduce<DW>(e, L.dbuf, OpSum());
-    const double p = e / zt;
+    double p[PER], zt = 0.0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        p[k] = 0.0;
+        if (id[k] >= 0 && !(t[k] == -INFINITY))
+            p[k] = tmax == INFINITY ? (t[k] == INFINITY ? 1.0 : t[k] != t[k] ? (double)t[k] : 0.0)
+                                    : exp(((double)t[k] - (double)tmax) * a.inv_tau);
+        zt += p[k];
+    }
+    zt = block_reduce<DW>(zt, L.dbuf, OpSum());
+#pragma unroll
+    for (int k = 0; k < PER; ++k) p[k] /= zt;
 
     // the row's maximum and sum
     float m = -INFINITY;
-    for (int64_t i = tid; i < a.N; i += DT) m = fmaxf(m, row_value(z[i]));
-    __syncthreads();
-    m = block_reduce<DW>(m, L.fbuf, OpMax());
-    float s = 0.f;
-    for (int64_t i = tid; i < a.N; i += DT) s += exp_of(row_value(z[i]) - m, chi, clo);
-    const double Z = block_reduce<DW>((double)s, L.dbuf2, OpSum());
+    double Z;
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const bool in = (int64_t)(j * DT + tid) < whole;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                x[j][e] = in ? row_value((T)raw[j][e]) : -INFINITY;
+                m = fmaxf(m, x[j][e]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) m = fmaxf(m, tail[e]);
+        m = block_reduce<DW>(m, L.fbuf2, OpMax());
+        float s[V] = {};
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                x[j][e] = exp_of(x[j][e] - m, chi, clo);
+                s[e] += x[j][e];
+            }
+        double sum = 0.0;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            tail[e] = exp_of(tail[e] - m, chi, clo);
+            sum += (double)(s[e] + tail[e]);
+        }
+        // (a row of -inf alone is NaN: so is every difference from its maximum)
+        Z = block_reduce<DW>(sum, L.dbuf2, OpSum());
+    } else {
+        // running maximum and sum of each thread, then of all
+        float s = 0.f;
+        auto add = [&](const float (&y)[V]) __attribute__((always_inline)) {
+            float top = y[0];
+#pragma unroll
+            for (int e = 1; e < V; ++e) top = fmaxf(top, y[e]);
+            if (top > m) {
+                s *= exp_of(m - top, chi, clo);
+                m = top;
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) s += y[e] == -INFINITY ? 0.f : exp_of(y[e] - m, chi, clo);
+        };
+#pragma unroll 4
+        for (int64_t i = tid; i < whole; i += DT) {
+            const vec r = *reinterpret_cast<const vec*>(z + i * V);
+            float y[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = row_value((T)r[e]);
+            add(y);
+        }
+        add(tail);
+        const float mine = m;
+        m = block_reduce<DW>(m, L.fbuf2, OpMax());
+        // (s is NaN where a score is: the factor must not hide it)
+        Z = block_reduce<DW>(s == 0.f && m > -INFINITY ? 0.0 : (double)(s * exp_of(mine - m, chi, clo)), L.dbuf2, OpSum());
+    }
 
     if (a.loss) {
         double l = 0.0;
-        if (p > 0.0 || p != p) {
-            const double logp = (tmax == INFINITY ? 0.0 : ((double)t - (double)tmax) * inv_tau) - log(zt);
-            const double logq = ((double)zj - (double)m) * inv_tau - log(Z);
-            l = p * (logp - logq);
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (p[k] > 0.0 || p[k] != p[k]) {
+                const double logp = (tmax == INFINITY ? 0.0 : ((double)t[k] - (double)tmax) * a.inv_tau) - log(zt);
+                const double logq = ((double)zj[k] - (double)m) * a.inv_tau - log(Z);
+                l += p[k] * (logp - logq);
+            }
         }
-        __syncthreads();
-        l = block_reduce<DW>(l, L.dbuf, OpSum());
-        if (tid == 0) a.loss[b] = empty ? 0.f : (float)(l * (double)a.tau * (double)a.tau);
+        l = block_reduce<DW>(l, L.dbuf3, OpSum());
+        if (tid == 0) a.loss[b] = empty ? 0.f : (float)(l * a.tau * a.tau);
     }
     if (!g) return;
 
     const float w = a.weight ? a.weight[b] : 1.f;
+    const double wt = (double)w * a.tau;
     // a row without a target, or without weight, has no gradient
-    if (empty || w == 0.f) {
-        for (int64_t i = tid; i < a.N; i += DT) g[i] = row_element<T>(0.f);
-        return;
-    }
+    const bool zero = empty || w == 0.f;
+    const float f = zero ? 0.f : (float)(zt == zt ? wt / Z : zt);
     // entries of one entity add up, in fixed point, so that their order does
     // not matter; the thread that opened the entity's slot writes its entry
-    int slot = -1;
-    if (id >= 0 && zt == zt) {
-        const unsigned long long fixed = (unsigned long long)(p * 0x1p62);
-        int at = (int)(((uint32_t)id * 2654435769u) >> 21);
-        for (;;) {
-            const int32_t was = atomicCAS(&L.key[at], -1, id);
-            if (was == -1) slot = at;
-            if (was == -1 || was == id) break;
-            at = (at + 1) & (kHash - 1);
+    int slot[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        slot[k] = -1;
+        if (id[k] >= 0 && zt == zt && !zero) {
+            const unsigned long long fixed = (unsigned long long)(p[k] * 0x1p62);
+            uint32_t at = ((uint32_t)id[k] * 2654435769u) >> 16 & (uint32_t)(slots - 1);
+            for (;;) {
+                const int32_t was = atomicCAS(&L.key[at], -1, id[k]);
+                if (was == -1) slot[k] = (int)at;
+                if (was == -1 || was == id[k]) break;
+                at = (at + 1) & (uint32_t)(slots - 1);
+            }
+            atomicAdd(&L.sum[at], fixed);
         }
-        atomicAdd(&L.sum[at], fixed);
     }
-    const double wt = (double)w * (double)a.tau;
-    const float f = (float)(zt == zt ? wt / Z : zt);
-    for (int64_t i = tid; i < a.N; i += DT) g[i] = row_element<T>(exp_of(row_value(z[i]) - m, chi, clo) * f);
+    auto store = [&](int64_t i, const float (&y)[V]) __attribute__((always_inline)) {
+        vec r;
+#pragma unroll
+        for (int e = 0; e < V; ++e) r[e] = row_element<T>(zero ? 0.f : y[e] * f);
+        *reinterpret_cast<vec*>(g + i * V) = r;
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if ((int64_t)(j * DT + tid) < whole) store(j * DT + tid, x[j]);
+    } else {
+#pragma unroll 4
+        for (int64_t i = tid; i < whole; i += DT) {
+            const vec r = *reinterpret_cast<const vec*>(z + i * V);
+            float y[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = exp_of(row_value((T)r[e]) - m, chi, clo);
+            store(i, y);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) tail[e] = exp_of(tail[e] - m, chi, clo);
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (last && whole * V + e < N) g[whole * V + e] = row_element<T>(zero ? 0.f : tail[e] * f);
+    // the entries of the list, behind the row's own
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
     __syncthreads();
-    if (slot >= 0) {
-        const double q = (double)exp_of(zj - m, chi, clo) / Z;
-        g[id] = row_element<T>((float)(wt * (q - (double)L.sum[slot] * 0x1p-62)));
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        if (slot[k] >= 0) {
+            const double q = (double)exp_of(zj[k] - m, chi, clo) / Z;
+            g[id[k]] = row_element<T>((float)(wt * (q - (double)L.sum[slot[k]] * 0x1p-62)));
+        }
     }
 }
 
+namespace {
+
+template <typename T>
+void launch(const DistillArgs& a, hipStream_t s)
+{
+    const double c = 1.4426950408889634074 / a.tau;
+    const float chi = (float)c;
+    const float clo = chi > 0.f && chi < INFINITY ? (float)((c - (double)chi) / c) : 0.f;
+    int slots = 64;
+    while (slots < 2 * a.k) slots <<= 1;
+    constexpr int V = RowVec<T>::n;
+    auto go = [&](auto kernel, int threads) {
+        hipLaunchKernelGGL(kernel, dim3(a.batch), dim3(threads), 0, s, a, chi, clo, slots);
+    };
+    // the row in registers where it fits: 16 scores a thread up to 16,384, which
+    // leaves several rows to a compute unit; 128 up to 65,536
+    if (a.N <= 4096) go(k_distill<T, 256, 16 / V>, 256);
+    else if (a.N <= 16384) go(k_distill<T, 1024, 16 / V>, 1024);
+    else if (a.N <= 65536) go(k_distill<T, 512, 128 / V>, 512);
+    else go(k_distill<T, 1024, 0>, 1024);
+}
+
+}  // namespace
+
 void launch_distill(const DistillArgs& a, hipStream_t s)
 {
-    const double c = 1.4426950408889634074 / (double)a.tau;
-    const float chi = (float)c;
-    const float clo = (float)((c - (double)chi) / c);
-    if (a.dtype == KGQ_BF16)
-        hipLaunchKernelGGL(k_distill<uint16_t>, dim3(a.batch), dim3(DT), 0, s, a, chi, clo);
-    else
-        hipLaunchKernelGGL(k_distill<float>, dim3(a.batch), dim3(DT), 0, s, a, chi, clo);
+    if (a.dtype == KGQ_BF16) launch<uint16_t>(a, s);
+    else launch<float>(a, s);
 }
 
 }  // namespace kgq

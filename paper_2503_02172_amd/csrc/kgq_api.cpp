@@ -1786,7 +1786,7 @@ kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t 
 }
 
 kgq_status kgq_distill(kgq_handle* h, int32_t batch, const void* scores, int32_t dtype, int64_t ld, int32_t k,
-                       const int32_t* teacher_idx, const float* teacher_score, float temperature,
+                       const int32_t* teacher_idx, const float* teacher_score, double temperature,
                        const float* row_weight, float* out_loss, void* out_grad, int64_t ld_grad, void* stream)
 {
     if (!h) return KGQ_E_INVALID_ARG;
@@ -1799,14 +1799,14 @@ kgq_status kgq_distill(kgq_handle* h, int32_t batch, const void* scores, int32_t
     if (ld < N || (out_grad && ld_grad < N))
         return fail(h, KGQ_E_INVALID_ARG, "ld and ld_grad must be >= n_entities");
     if (k < 1 || k > kMaxK) return fail(h, KGQ_E_INVALID_ARG, "k outside [1, KGQ_MAX_K]");
-    if (!(temperature > 0.f && temperature <= 3.4028234e38f))
-        return fail(h, KGQ_E_INVALID_ARG, "temperature must be finite and > 0");
+    if (!(temperature >= 1e-30 && temperature <= 1e30))
+        return fail(h, KGQ_E_INVALID_ARG, "temperature outside [1e-30, 1e30]");
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     DeviceGuard dev;
     Lane* L = nullptr;
     kgq_status st = rows_begin(h, dev, s, &L);
     if (st != KGQ_OK) return st;
-    launch_distill({scores, dtype, ld, N, batch, k, teacher_idx, teacher_score, temperature, row_weight, out_loss,
+    launch_distill({scores, dtype, ld, N, batch, k, teacher_idx, teacher_score, temperature, 1.0 / temperature, row_weight, out_loss,
                     out_grad, ld_grad, L ? L->dflag : nullptr},
                    s);
     return rows_end(h, L, s, "an entity of a teacher's list is out of range");

@@ -496,7 +496,7 @@ struct DistillArgs {
     const void* scores; int dtype; int64_t ld; int64_t N;
     int batch, k;
     const int32_t* idx; const float* teacher;                    // [batch x k]
-    float tau; const float* weight;    // [batch] or nullptr (1)
+    double tau, inv_tau; const float* weight;                    // [batch] or nullptr (1)
     float* loss;                       // [batch] or nullptr
     void* grad; int64_t ld_grad;       // of dtype, or nullptr
     int* flag;

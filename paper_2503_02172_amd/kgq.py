@@ -95,7 +95,7 @@ def lib() -> ctypes.CDLL:
         "kgq_sample": ([vp, i32, vp, i32, i64, ctypes.POINTER(Sampling), vp, i32, vp, vp, vp,
                         ctypes.c_size_t, vp], i32),
         "kgq_sample_workspace": ([vp, i32, ctypes.POINTER(ctypes.c_size_t)], i32),
-        "kgq_distill": ([vp, i32, vp, i32, i64, i32, vp, vp, ctypes.c_float, vp, vp, vp, i64, vp], i32),
+        "kgq_distill": ([vp, i32, vp, i32, i64, i32, vp, vp, ctypes.c_double, vp, vp, vp, i64, vp], i32),
         "kgq_embed": ([vp, vp, i32, i64, i32, i64, vp, i32, ctypes.c_float, vp, i32, i64, vp], i32),
         "kgq_embed_grad_workspace": ([vp, i64, i32, i32, ctypes.POINTER(ctypes.c_size_t)], i32),
         "kgq_embed_grad": ([vp, vp, i32, i32, i32, i64, vp, i64, ctypes.c_float, vp, i32, i64, i32, vp,

@@ -43,7 +43,7 @@ def call(eng, z, idx, t, tau, w, dtype="f32", pad=0, out=None, **kw):
 def check(eng, z, idx, t, tau, w, what, dtype="f32", **kw):
     loss, grad, used = call(eng, z, idx, t, tau, w, dtype, **kw)
     ww = np.ones(len(z)) if w is None else w.astype(np.float64)
-    rl, rg, lb, gb = R.distill(used, idx, t, float(np.float32(tau)), ww)
+    rl, rg, lb, gb = R.distill(used, idx, t, tau, ww)
     if dtype == "bf16":
         gb = gb + R.U16 * (np.abs(rg) + gb)
     for name, got, ref, bound in (("loss", loss, rl, lb), ("grad", grad, rg, gb)):

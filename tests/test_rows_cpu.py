@@ -56,7 +56,7 @@ def test_distill_refusals(eng):
     assert distill(eng) == -5 and distill(eng, grad=None, ldg=0) == -5 and distill(eng, loss=None) == -5
     assert distill(None) == -1
     for bad in (dict(batch=0), dict(scores=None), dict(dtype=-1), dict(ld=49), dict(ldg=49), dict(k=0), dict(k=1025),
-                dict(idx=None), dict(score=None), dict(tau=0.0), dict(tau=-1.0), dict(tau=float("nan")),
+                dict(idx=None), dict(score=None), dict(tau=0.0), dict(tau=-1.0), dict(tau=float("nan")), dict(tau=1e-31),
                 dict(tau=float("inf")), dict(loss=None, grad=None)):
         assert distill(eng, **bad) == -1, bad
 
