@@ -33,9 +33,9 @@ template <int DW>
 struct DistillLds {
     int32_t key[kHash];
     unsigned long long sum[kHash];
-    float fbuf[DW], fbuf2[DW];
-    double dbuf[DW], dbuf2[DW], dbuf3[DW];
-    int any;
+    float top[DW], list_top[DW];
+    int any[DW];
+    double sum_exp[DW], list_sum[DW], loss[DW];
 };
 
 // V elements at p.
@@ -43,19 +43,38 @@ template <typename T, int V>
 struct Elements {
     typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 };
+// The same 16 bytes as words, and element e of them.
+template <typename T>
+struct Words;
+template <>
+struct Words<float> {
+    typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <>
+struct Words<uint16_t> {
+    typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(2)));
+};
+template <typename T, typename W>
+__device__ __forceinline__ float word_value(const W& w, int e)
+{
+    if (sizeof(T) == 4) return __uint_as_float(w[e]);
+    return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+}
 
 }  // namespace
 
 // One workgroup per row. NV > 0: the row's scores in registers, NV vectors of
-// 16 bytes a thread and one more for the row's end; NV = 0: the row is read
-// twice.
-template <typename T, int DT, int NV>
-__global__ __launch_bounds__(DT) void k_distill(DistillArgs a, float chi, float clo, int slots)
+// 16 bytes a thread and the row's end beside them; their exponentials take the
+// scores' place, or (KEEP false, bfloat16: half the registers, and twice the
+// rows in flight) are computed again for the gradient. NV = 0: the row is read
+// twice. Three barriers: behind the maxima, the sums, and the row's stores.
+template <typename T, int DT, int NV, bool KEEP, int WAVES>
+__global__ __launch_bounds__(DT, WAVES) void k_distill(DistillArgs a, float chi, float clo, int slots)
 {
     constexpr int V = RowVec<T>::n, DW = DT / 64, PER = kMaxK / DT;
     typedef typename Elements<T, V>::vec vec;
     __shared__ DistillLds<DW> L;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, wave = tid >> 6;
     const int64_t b = blockIdx.x, N = a.N;
     const T* z = reinterpret_cast<const T*>(a.scores) + b * a.ld;
     T* g = a.grad ? reinterpret_cast<T*>(a.grad) + b * a.ld_grad : nullptr;
@@ -73,13 +92,13 @@ __global__ __launch_bounds__(DT) void k_distill(DistillArgs a, float chi, float 
     // count as -inf), and the last elements, one by one, in one thread
     const int64_t whole = N / V;
     const bool last = tid == (int)(whole % DT);
-    vec raw[NV > 0 ? NV : 1];
-    float x[NV > 0 ? NV : 1][V], tail[V];
+    typename Words<T>::vec raw[NV > 0 ? NV : 1];
+    float x[NV > 0 && KEEP ? NV : 1][V], tail[V];
     if constexpr (NV > 0) {
         if (whole > 0) {
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-                raw[j] = *reinterpret_cast<const vec*>(z + min((int64_t)(j * DT + tid), whole - 1) * V);
+                raw[j] = *reinterpret_cast<const typename Words<T>::vec*>(z + min((int64_t)(j * DT + tid), whole - 1) * V);
         }
     }
 #pragma unroll
@@ -89,9 +108,8 @@ __global__ __launch_bounds__(DT) void k_distill(DistillArgs a, float chi, float 
         L.key[i] = -1;
         L.sum[i] = 0ull;
     }
-    if (tid == 0) L.any = 0;
-    __syncthreads();
     float tmax = -INFINITY;
+    bool any = false;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         if (id[k] >= N || id[k] < -1) {
@@ -101,72 +119,40 @@ __global__ __launch_bounds__(DT) void k_distill(DistillArgs a, float chi, float 
         zj[k] = 0.f;
         if (id[k] >= 0) {
             zj[k] = row_value(z[id[k]]);
-            if (!(t[k] == -INFINITY)) L.any = 1;       // (a NaN is a target: it makes the row NaN)
+            any |= !(t[k] == -INFINITY);               // (a NaN is a target: it makes the row NaN)
         } else {
             t[k] = -INFINITY;
         }
         tmax = fmaxf(tmax, t[k]);
     }
-    tmax = block_reduce<DW>(tmax, L.fbuf, OpMax());
-    const bool empty = L.any == 0;
-    double p[PER], zt = 0.0;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        p[k] = 0.0;
-        if (id[k] >= 0 && !(t[k] == -INFINITY))
-            p[k] = tmax == INFINITY ? (t[k] == INFINITY ? 1.0 : t[k] != t[k] ? (double)t[k] : 0.0)
-                                    : exp(((double)t[k] - (double)tmax) * a.inv_tau);
-        zt += p[k];
-    }
-    zt = block_reduce<DW>(zt, L.dbuf, OpSum());
-#pragma unroll
-    for (int k = 0; k < PER; ++k) p[k] /= zt;
-
-    // the row's maximum and sum
-    float m = -INFINITY;
-    double Z;
+    // the maxima
+    auto value = [&](int j, int e) __attribute__((always_inline)) {
+        return (int64_t)(j * DT + tid) < whole ? word_value<T>(raw[j], e) : -INFINITY;
+    };
+    float m = -INFINITY, part = 0.f;
     if constexpr (NV > 0) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const bool in = (int64_t)(j * DT + tid) < whole;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                x[j][e] = in ? row_value((T)raw[j][e]) : -INFINITY;
-                m = fmaxf(m, x[j][e]);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e) m = fmaxf(m, tail[e]);
-        m = block_reduce<DW>(m, L.fbuf2, OpMax());
-        float s[V] = {};
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                x[j][e] = exp_of(x[j][e] - m, chi, clo);
-                s[e] += x[j][e];
+                const float y = value(j, e);
+                if (KEEP) x[j][e] = y;
+                m = fmaxf(m, y);
             }
-        double sum = 0.0;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            tail[e] = exp_of(tail[e] - m, chi, clo);
-            sum += (double)(s[e] + tail[e]);
-        }
-        // (a row of -inf alone is NaN: so is every difference from its maximum)
-        Z = block_reduce<DW>(sum, L.dbuf2, OpSum());
+        for (int e = 0; e < V; ++e) m = fmaxf(m, tail[e]);
     } else {
-        // running maximum and sum of each thread, then of all
-        float s = 0.f;
+        // (and each thread's sum relative to its own)
         auto add = [&](const float (&y)[V]) __attribute__((always_inline)) {
             float top = y[0];
 #pragma unroll
             for (int e = 1; e < V; ++e) top = fmaxf(top, y[e]);
             if (top > m) {
-                s *= exp_of(m - top, chi, clo);
+                part *= exp_of(m - top, chi, clo);
                 m = top;
             }
 #pragma unroll
-            for (int e = 0; e < V; ++e) s += y[e] == -INFINITY ? 0.f : exp_of(y[e] - m, chi, clo);
+            for (int e = 0; e < V; ++e) part += y[e] == -INFINITY ? 0.f : exp_of(y[e] - m, chi, clo);
         };
 #pragma unroll 4
         for (int64_t i = tid; i < whole; i += DT) {
@@ -177,26 +163,97 @@ __global__ __launch_bounds__(DT) void k_distill(DistillArgs a, float chi, float 
             add(y);
         }
         add(tail);
-        const float mine = m;
-        m = block_reduce<DW>(m, L.fbuf2, OpMax());
-        // (s is NaN where a score is: the factor must not hide it)
-        Z = block_reduce<DW>(s == 0.f && m > -INFINITY ? 0.0 : (double)(s * exp_of(mine - m, chi, clo)), L.dbuf2, OpSum());
     }
-
-    if (a.loss) {
-        double l = 0.0;
+    const float mine = m;
+    m = wave_reduce(m, OpMax());
+    tmax = wave_reduce(tmax, OpMax());
+    any = __builtin_amdgcn_ballot_w64(any) != 0;
+    if ((tid & 63) == 0) {
+        L.top[wave] = m;
+        L.list_top[wave] = tmax;
+        L.any[wave] = any;
+    }
+    __syncthreads();
+    bool empty = true;
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            if (p[k] > 0.0 || p[k] != p[k]) {
-                const double logp = (tmax == INFINITY ? 0.0 : ((double)t[k] - (double)tmax) * a.inv_tau) - log(zt);
-                const double logq = ((double)zj[k] - (double)m) * a.inv_tau - log(Z);
-                l += p[k] * (logp - logq);
-            }
-        }
-        l = block_reduce<DW>(l, L.dbuf3, OpSum());
-        if (tid == 0) a.loss[b] = empty ? 0.f : (float)(l * a.tau * a.tau);
+    for (int w = 0; w < DW; ++w) {
+        m = fmaxf(m, L.top[w]);
+        tmax = fmaxf(tmax, L.list_top[w]);
+        empty &= !L.any[w];
     }
-    if (!g) return;
+    // (what was computed of the scores is not to be kept, where they are)
+    auto again = [&]() __attribute__((always_inline)) {
+        if constexpr (NV > 0 && !KEEP) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t u = raw[j][k];
+                    asm volatile("" : "+v"(u));
+                    raw[j][k] = u;
+                }
+        }
+    };
+    // the sums
+    double p[PER], zt = 0.0, Z = 0.0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        p[k] = 0.0;
+        if (id[k] >= 0 && !(t[k] == -INFINITY))
+            p[k] = tmax == INFINITY ? (t[k] == INFINITY ? 1.0 : t[k] != t[k] ? (double)t[k] : 0.0)
+                                    : exp(((double)t[k] - (double)tmax) * a.inv_tau);
+        zt += p[k];
+    }
+    if constexpr (NV > 0) {
+        float s[V] = {};
+        again();
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float y = exp_of((KEEP ? x[j][e] : value(j, e)) - m, chi, clo);
+                if (KEEP) x[j][e] = y;
+                s[e] += y;
+            }
+        // (a row of -inf alone is NaN: so is every difference from its maximum)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            tail[e] = exp_of(tail[e] - m, chi, clo);
+            Z += (double)(s[e] + tail[e]);
+        }
+    } else {
+        // (NaN where a score is: the factor must not hide it)
+        Z = part == 0.f && m > -INFINITY ? 0.0 : (double)(part * exp_of(mine - m, chi, clo));
+#pragma unroll
+        for (int e = 0; e < V; ++e) tail[e] = exp_of(tail[e] - m, chi, clo);
+    }
+    Z = wave_reduce(Z, OpSum());
+    zt = wave_reduce(zt, OpSum());
+    if ((tid & 63) == 0) {
+        L.sum_exp[wave] = Z;
+        L.list_sum[wave] = zt;
+    }
+    __syncthreads();
+    Z = zt = 0.0;
+#pragma unroll
+    for (int w = 0; w < DW; ++w) {
+        Z += L.sum_exp[w];
+        zt += L.list_sum[w];
+    }
+    double l = 0.0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        p[k] /= zt;
+        if (a.loss && (p[k] > 0.0 || p[k] != p[k])) {
+            const double logp = (tmax == INFINITY ? 0.0 : ((double)t[k] - (double)tmax) * a.inv_tau) - log(zt);
+            const double logq = ((double)zj[k] - (double)m) * a.inv_tau - log(Z);
+            l += p[k] * (logp - logq);
+        }
+    }
+    if (a.loss) {
+        l = wave_reduce(l, OpSum());
+        if ((tid & 63) == 0) L.loss[wave] = l;
+    }
 
     const float w = a.weight ? a.weight[b] : 1.f;
     const double wt = (double)w * a.tau;
@@ -209,7 +266,7 @@ __global__ __launch_bounds__(DT) void k_distill(DistillArgs a, float chi, float 
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         slot[k] = -1;
-        if (id[k] >= 0 && zt == zt && !zero) {
+        if (g && id[k] >= 0 && zt == zt && !zero) {
             const unsigned long long fixed = (unsigned long long)(p[k] * 0x1p62);
             uint32_t at = ((uint32_t)id[k] * 2654435769u) >> 16 & (uint32_t)(slots - 1);
             for (;;) {
@@ -227,28 +284,39 @@ __global__ __launch_bounds__(DT) void k_distill(DistillArgs a, float chi, float 
         for (int e = 0; e < V; ++e) r[e] = row_element<T>(zero ? 0.f : y[e] * f);
         *reinterpret_cast<vec*>(g + i * V) = r;
     };
-    if constexpr (NV > 0) {
+    if (g) {
+        again();
+        if constexpr (NV > 0) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if ((int64_t)(j * DT + tid) < whole) store(j * DT + tid, x[j]);
-    } else {
+            for (int j = 0; j < NV; ++j) {
+                float y[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = KEEP ? x[j][e] : exp_of(value(j, e) - m, chi, clo);
+                if ((int64_t)(j * DT + tid) < whole) store(j * DT + tid, y);
+            }
+        } else {
 #pragma unroll 4
-        for (int64_t i = tid; i < whole; i += DT) {
-            const vec r = *reinterpret_cast<const vec*>(z + i * V);
-            float y[V];
+            for (int64_t i = tid; i < whole; i += DT) {
+                const vec r = *reinterpret_cast<const vec*>(z + i * V);
+                float y[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) y[e] = exp_of(row_value((T)r[e]) - m, chi, clo);
-            store(i, y);
+                for (int e = 0; e < V; ++e) y[e] = exp_of(row_value((T)r[e]) - m, chi, clo);
+                store(i, y);
+            }
         }
 #pragma unroll
-        for (int e = 0; e < V; ++e) tail[e] = exp_of(tail[e] - m, chi, clo);
+        for (int e = 0; e < V; ++e)
+            if (last && whole * V + e < N) g[whole * V + e] = row_element<T>(zero ? 0.f : tail[e] * f);
     }
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-        if (last && whole * V + e < N) g[whole * V + e] = row_element<T>(zero ? 0.f : tail[e] * f);
     // the entries of the list, behind the row's own
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
     __syncthreads();
+    if (a.loss && tid == 0) {
+        l = 0.0;
+#pragma unroll
+        for (int v = 0; v < DW; ++v) l += L.loss[v];
+        a.loss[b] = empty ? 0.f : (float)(l * a.tau * a.tau);
+    }
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         if (slot[k] >= 0) {
@@ -272,12 +340,14 @@ void launch(const DistillArgs& a, hipStream_t s)
     auto go = [&](auto kernel, int threads) {
         hipLaunchKernelGGL(kernel, dim3(a.batch), dim3(threads), 0, s, a, chi, clo, slots);
     };
-    // the row in registers where it fits: 16 scores a thread up to 16,384, which
-    // leaves several rows to a compute unit; 128 up to 65,536
-    if (a.N <= 4096) go(k_distill<T, 256, 16 / V>, 256);
-    else if (a.N <= 16384) go(k_distill<T, 1024, 16 / V>, 1024);
-    else if (a.N <= 65536) go(k_distill<T, 512, 128 / V>, 512);
-    else go(k_distill<T, 1024, 0>, 1024);
+    // the row in registers where it fits: 16 or 32 scores a thread up to 16,384,
+    // which leaves several rows to a compute unit; 128 up to 65,536, one row a
+    // compute unit (bfloat16: two)
+    constexpr bool half = sizeof(T) == 2;
+    if (a.N <= 4096) go(k_distill<T, 256, 16 / V, true, 4>, 256);
+    else if (a.N <= 16384) go(k_distill<T, 512, 32 / V, true, 4>, 512);
+    else if (a.N <= 65536) go(k_distill<T, 512, 128 / V, !half, half ? 4 : 2>, 512);
+    else go(k_distill<T, 1024, 0, false, 4>, 1024);
 }
 
 }  // namespace
