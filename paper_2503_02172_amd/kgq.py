@@ -357,21 +357,26 @@ class Engine:
 
     # -- drawing, distillation, embedding rows ----------------------------------
     def _rows_stream(self, stream, inputs):
-        """The call's torch stream; inputs' memory outlives the work on it."""
+        """(raw stream, allocator on it) of a call; with a stream of the
+        caller's, inputs' memory outlives the work on it."""
         import torch
-        dev = torch.device("cuda", self.device)
         if stream is None:
-            return torch.cuda.current_stream(dev)
+            return torch.cuda.current_stream(self.device).cuda_stream, torch.empty
+        dev = torch.device("cuda", self.device)
         ts = torch.cuda.ExternalStream(stream, device=dev) if isinstance(stream, int) else stream
         for t in inputs:
             if t is not None:
                 t.record_stream(ts)
-        return ts
+
+        def empty(*shape, **kw):
+            with torch.cuda.stream(ts):
+                return torch.empty(*shape, **kw)
+        return ts.cuda_stream, empty
 
     def _matrix(self, call: str, name: str, t, width: Optional[int] = None):
         """(dtype, row stride) of a float32 or bfloat16 matrix on the handle's device."""
         import torch
-        dt = {torch.float32: F32, torch.bfloat16: BF16}.get(t.dtype)
+        dt = F32 if t.dtype == torch.float32 else BF16 if t.dtype == torch.bfloat16 else None
         if dt is None or t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
             raise TypeError(f"{call}: {name} must be a float32 or bfloat16 CUDA matrix with unit column stride")
         if t.device.index != self.device:
@@ -415,13 +420,12 @@ class Engine:
         rc = lib().kgq_sample_workspace(self.h, B, ctypes.byref(need))
         if rc != OK:
             raise KgqError(rc, "sample: batch outside [1, 2^20]")
-        ts = self._rows_stream(stream, kept)
-        with torch.cuda.stream(ts):
-            idx = torch.empty(u.shape, dtype=torch.int32, device=u.device)
-            lp = torch.empty(u.shape, dtype=torch.float32, device=u.device) if logp else None
-            ws = torch.empty(need.value, dtype=torch.uint8, device=u.device)
+        raw, empty = self._rows_stream(stream, kept)
+        idx = empty(u.shape, dtype=torch.int32, device=u.device)
+        lp = empty(u.shape, dtype=torch.float32, device=u.device) if logp else None
+        ws = empty(need.value, dtype=torch.uint8, device=u.device)
         self._check(lib().kgq_sample(self.h, B, _ptr(scores), dt, ld, ctypes.byref(how), _ptr(u), u.shape[1],
-                                     _ptr(idx), _ptr(lp), _ptr(ws), need.value, _stream(ts)))
+                                     _ptr(idx), _ptr(lp), _ptr(ws), need.value, raw))
         return idx, lp
 
     def distill(self, scores, idx, score, temperature: float = 1.0, weight=None, loss: bool = True,
@@ -450,15 +454,14 @@ class Engine:
                    ((scores, ld), (out, ld_grad))]
             if not same and out.data_ptr() < end[0] and scores.data_ptr() < end[1]:
                 raise ValueError("distill: out overlaps scores and is not the same matrix")
-        ts = self._rows_stream(stream, (scores, idx, score, weight, out))
-        with torch.cuda.stream(ts):
-            ls = torch.empty(B, dtype=torch.float32, device=scores.device) if loss else None
-            if grad and out is None:
-                out = torch.empty((B, self.n_entities), dtype=scores.dtype, device=scores.device)
-                ld_grad = self.n_entities
+        raw, empty = self._rows_stream(stream, (scores, idx, score, weight, out))
+        ls = empty(B, dtype=torch.float32, device=scores.device) if loss else None
+        if grad and out is None:
+            out = empty((B, self.n_entities), dtype=scores.dtype, device=scores.device)
+            ld_grad = self.n_entities
         g = out if grad else None
         self._check(lib().kgq_distill(self.h, B, _ptr(scores), dt, ld, idx.shape[1], _ptr(idx), _ptr(score),
-                                      temperature, _ptr(weight), _ptr(ls), _ptr(g), ld_grad, _stream(ts)))
+                                      temperature, _ptr(weight), _ptr(ls), _ptr(g), ld_grad, raw))
         return ls, g
 
     def embed(self, table, ids, scale: float = 1.0, dtype=None, stream=None):
@@ -472,11 +475,10 @@ class Engine:
         dtype = dtype or table.dtype
         if dtype not in (torch.float32, torch.bfloat16):
             raise TypeError("embed: dtype must be float32 or bfloat16")
-        ts = self._rows_stream(stream, (table, ids))
-        with torch.cuda.stream(ts):
-            out = torch.empty(tuple(ids.shape) + (d,), dtype=dtype, device=table.device)
+        raw, empty = self._rows_stream(stream, (table, ids))
+        out = empty(tuple(ids.shape) + (d,), dtype=dtype, device=table.device)
         self._check(lib().kgq_embed(self.h, _ptr(table), dt, table.shape[0], d, ld, _ptr(ids), ids.numel(), scale,
-                                    _ptr(out), F32 if dtype == torch.float32 else BF16, d, _stream(ts)))
+                                    _ptr(out), F32 if dtype == torch.float32 else BF16, d, raw))
         return out
 
     def embed_grad(self, grad, ids, rows: int, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False,
@@ -507,13 +509,12 @@ class Engine:
         need = ctypes.c_size_t()
         if lib().kgq_embed_grad_workspace(self.h, rows, d, n, ctypes.byref(need)) != OK:
             raise ValueError("embed_grad: rows, d or the number of ids is out of range")
-        ts = self._rows_stream(stream, (grad, ids, out))
-        with torch.cuda.stream(ts):
-            if out is None:
-                out = torch.empty((rows, d), dtype=dtype, device=grad.device)
-            ws = torch.empty(need.value, dtype=torch.uint8, device=grad.device)
+        raw, empty = self._rows_stream(stream, (grad, ids, out))
+        if out is None:
+            out = empty((rows, d), dtype=dtype, device=grad.device)
+        ws = empty(need.value, dtype=torch.uint8, device=grad.device)
         self._check(lib().kgq_embed_grad(self.h, _ptr(grad), dt, n, d, ld, _ptr(ids), rows, scale, _ptr(out), odt,
-                                         ld_out, int(accumulate), _ptr(ws), need.value, _stream(ts)))
+                                         ld_out, int(accumulate), _ptr(ws), need.value, raw))
         return out
 
     # -- profiling ------------------------------------------------------------
