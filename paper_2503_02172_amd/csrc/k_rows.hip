@@ -44,7 +44,7 @@ __device__ __forceinline__ void load_columns(const T* p, int left, float (&x)[V]
     }
 }
 // p[j] = scale x[j] (+ p[j])
-template <int V, typename O>
+template <int V, bool STREAM = false, typename O>
 __device__ __forceinline__ void store_columns(O* p, int left, const float (&x)[V], float scale, bool accumulate)
 {
     typedef O vec __attribute__((ext_vector_type(V), aligned(sizeof(O))));
@@ -54,7 +54,8 @@ __device__ __forceinline__ void store_columns(O* p, int left, const float (&x)[V
 #pragma unroll
         for (int j = 0; j < V; ++j)
             y[j] = row_element<O>(accumulate ? x[j] * scale + row_value((O)old[j]) : x[j] * scale);
-        *reinterpret_cast<vec*>(p) = y;
+        if (STREAM) __builtin_nontemporal_store(y, reinterpret_cast<vec*>(p));
+        else *reinterpret_cast<vec*>(p) = y;
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs a, int per, int ve
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (t[u] >= 0) store_columns<V>(out + t[u] * a.ld_out + c[u], a.d - c[u], x[u], a.scale, false);
+            if (t[u] >= 0) store_columns<V, (U > 1)>(out + t[u] * a.ld_out + c[u], a.d - c[u], x[u], a.scale, false);
     }
 }
 
