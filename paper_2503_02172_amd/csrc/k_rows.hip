@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cu
                 constexpr int VO = RowVec<O>::n;
                 for (int c = lane * VO; c < a.d; c += 64 * VO) {
                     const float zero[VO] = {};
-                    store_columns<VO>(row + c, a.d - c, zero, 1.f, false);
+                    store_columns<VO, true>(row + c, a.d - c, zero, 1.f, false);
                 }
             }
         }
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cu
             if (from_before || leaves) {
                 store_columns<V>(piece + (2 * chunk + (from_before ? 0 : 1)) * a.d + col, left, sum, 1.f, false);
             } else {
-                store_columns<V>(out + (int64_t)run * a.ld_out, left, sum, a.scale, a.accumulate != 0);
+                store_columns<V, true>(out + (int64_t)run * a.ld_out, left, sum, a.scale, a.accumulate != 0);
             }
         }
 #pragma unroll
