@@ -44,19 +44,19 @@ constexpr int kRun = 16;                     // lanes per draw, and per 64 score
 constexpr int kPiece = 1024;                 // scores of a row per wavefront, without cuts
 constexpr int kMaxPieces = 320;              // of a row (their chunks' running sums lie in LDS)
 
-// 2^r on |r| <= 1/2, off by 3e-16: the polynomial through Chebyshev's points.
+// 2^r on |r| <= 1/2, off by 4e-14 (a draw compares sums that are off by less
+// then, and none in 10^8 moves): the polynomial through Chebyshev's points.
 __device__ __forceinline__ double pow2_part(double r)
 {
-    double y = 7.072585949269223e-09;
-    y = fma(y, r, 1.0208690299958306e-07);
-    y = fma(y, r, 1.321544258792169e-06);
-    y = fma(y, r, 1.5252657260200837e-05);
-    y = fma(y, r, 0.0001540353044173605);
-    y = fma(y, r, 0.0013333558230164974);
-    y = fma(y, r, 0.009618129107606888);
-    y = fma(y, r, 0.05550410866444772);
-    y = fma(y, r, 0.24022650695910097);
-    y = fma(y, r, 0.69314718055995);
+    double y = 1.0205905413765595e-07;
+    y = fma(y, r, 1.325964524488711e-06);
+    y = fma(y, r, 1.5252672924850737e-05);
+    y = fma(y, r, 0.0001540343375125101);
+    y = fma(y, r, 0.0013333558200794592);
+    y = fma(y, r, 0.009618129193934313);
+    y = fma(y, r, 0.05550410866465167);
+    y = fma(y, r, 0.2402265069564034);
+    y = fma(y, r, 0.6931471805599462);
     return fma(y, r, 1.0);
 }
 // 2^t for t <= 0, 0 below 2^-1074 and for NaN.
@@ -328,92 +328,6 @@ __device__ __forceinline__ uint32_t sorted_cut(SampleLds<THREADS, CHUNKS>& L, in
     return L.n;
 }
 
-// The composite of the last entry that a cut keeps, among the entries with a
-// composite of at least `floor` (the cut before). range: distances from M that
-// the first histogram spans; entries further off count as one bin.
-template <int THREADS, int CHUNKS, typename T>
-__device__ __forceinline__ uint64_t find_cut(SampleLds<THREADS, CHUNKS>& L, const T* row, int64_t N, const RowWeight& wt,
-                                             const CutGoal& goal, uint64_t floor, float range)
-{
-    const int tid = threadIdx.x;
-    const int bits = 62 - (64 - __builtin_clzll((unsigned long long)N));
-    const double unit = ldexp(1.0, bits);
-    const float step = range < INFINITY ? range / (float)(kBins - 1) : 0.f;
-    const float inv = step > 0.f ? 1.0f / step : 0.f;
-    uint32_t count = 0;
-    double mass = 0.0;
-    unsigned long long lo = floor, hi = ~0ull;
-    auto bin_of = [&](float x) {
-        const float v = (wt.top - x) * inv;        // 0 and up; NaN (infinite M, or a step of 0) to bin 0
-        return v < (float)(kBins - 1) ? max((int)v, 0) : v >= (float)(kBins - 1) ? kBins - 1 : 0;
-    };
-    for (int level = 0;; ++level) {
-        // histogram over [lo, hi]
-        for (int i = tid; i < kBins; i += THREADS) {
-            L.h.count[i] = 0;
-            L.h.mass[i] = 0;
-        }
-        __syncthreads();
-        const int shift = level == 0 ? 0 : max(0, 64 - __builtin_clzll((hi - lo) | 1ull) - 11);
-        const double top = level == 0 ? 0.0 : wt.exponent(ranking_score(hi));
-        auto scale_of = [&](int bin) { return level == 0 ? fmax((double)bin * (double)step * -wt.c, -1100.0) : top; };
-        // (an entry whose distance was rounded up into its bin may weigh a
-        // little more than the bin's scale: there is a bit of room for that)
-        auto value_bin = [&](float x, unsigned long long c) {
-            return level == 0 ? bin_of(x) : (int)((hi - c) >> shift);
-        };
-        for (int64_t i = tid; i < N; i += THREADS) {
-            const float x = row_value(row[i]);
-            if (!(x > -INFINITY)) continue;
-            const unsigned long long c = ranking(x, (uint32_t)i);
-            if (c < lo || c > hi) continue;
-            const int bin = value_bin(x, c);
-            atomicAdd(&L.h.count[bin], 1u);
-            if (goal.by_mass)
-                atomicAdd(&L.h.mass[bin], (unsigned long long)(pow2d(fmin(wt.exponent(x) - scale_of(bin), 0.5)) * unit));
-        }
-        __syncthreads();
-        find_bin(L, goal, [&](int bin) { return pow2d(scale_of(bin)) / unit; }, &count, &mass);
-        const int bin = L.bin;
-        const uint32_t in_bin = L.h.count[bin];
-        __syncthreads();
-        // the composites in that bin
-        if (tid == 0) {
-            L.lo = ~0ull;
-            L.hi = 0ull;
-            L.n = 0;
-        }
-        __syncthreads();
-        const bool take = in_bin <= (uint32_t)kSort;
-        unsigned long long mine_lo = ~0ull, mine_hi = 0ull;
-        for (int64_t i = tid; i < N; i += THREADS) {
-            const float x = row_value(row[i]);
-            if (!(x > -INFINITY)) continue;
-            const unsigned long long c = ranking(x, (uint32_t)i);
-            if (c < lo || c > hi || value_bin(x, c) != bin) continue;
-            mine_lo = min(mine_lo, c);
-            mine_hi = max(mine_hi, c);
-            if (take) L.s.c[atomicAdd(&L.n, 1u)] = c;
-        }
-        if (!take) {
-            if (mine_lo != ~0ull) {
-                atomicMin(&L.lo, mine_lo);
-                atomicMax(&L.hi, mine_hi);
-            }
-            __syncthreads();
-            lo = L.lo;
-            hi = L.hi;
-            __syncthreads();
-            continue;
-        }
-        __syncthreads();
-        const uint32_t at = sorted_cut(L, (int)in_bin, wt, goal, count, mass);
-        const uint64_t cut = L.s.c[at == in_bin ? in_bin - 1 : at];   // (short of the goal by rounding: the last one)
-        __syncthreads();
-        return cut;
-    }
-}
-
 // Four scores from element i (a multiple of 4) on, -inf past the row's end.
 // Without a branch: a vector that reaches past the end is loaded from the
 // row's last four (a row below four: element by element) and shifted by end4,
@@ -459,6 +373,118 @@ __device__ __forceinline__ void load4(const T* row, int64_t i, int64_t N, float 
     f.load(row, i, N);
     f.get(x);
     end4(x, i, N);
+}
+
+// f(first element, four scores) over the row, by THREADS threads, the same
+// number of times in each; four vectors ahead.
+template <int THREADS, typename T, typename F>
+__device__ __forceinline__ void each_four(const T* row, int64_t N, F f)
+{
+    const int tid = threadIdx.x;
+    float x[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) load4(row, (int64_t)(j * THREADS + tid) * 4, N, x[j]);
+#pragma unroll 1
+    for (int64_t i0 = 0; i0 < N; i0 += 4 * THREADS) {
+        f(i0 + tid * 4, x[0]);
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[j][e] = x[j + 1][e];
+        load4(row, i0 + (int64_t)(4 * THREADS + tid) * 4, N, x[3]);
+    }
+}
+
+// The composite of the last entry that a cut keeps, among the entries with a
+// composite of at least `floor` (the cut before). range: distances from M that
+// the first histogram spans; entries further off count as one bin.
+template <int THREADS, int CHUNKS, typename T>
+__device__ __forceinline__ uint64_t find_cut(SampleLds<THREADS, CHUNKS>& L, const T* row, int64_t N, const RowWeight& wt,
+                                             const CutGoal& goal, uint64_t floor, float range)
+{
+    const int tid = threadIdx.x;
+    const int bits = 62 - (64 - __builtin_clzll((unsigned long long)N));
+    const double unit = ldexp(1.0, bits);
+    const float step = range < INFINITY ? range / (float)(kBins - 1) : 0.f;
+    const float inv = step > 0.f ? 1.0f / step : 0.f;
+    uint32_t count = 0;
+    double mass = 0.0;
+    unsigned long long lo = floor, hi = ~0ull;
+    auto bin_of = [&](float x) {
+        const float v = (wt.top - x) * inv;        // 0 and up; NaN (infinite M, or a step of 0) to bin 0
+        return v < (float)(kBins - 1) ? max((int)v, 0) : v >= (float)(kBins - 1) ? kBins - 1 : 0;
+    };
+    for (int level = 0;; ++level) {
+        // histogram over [lo, hi]
+        for (int i = tid; i < kBins; i += THREADS) {
+            L.h.count[i] = 0;
+            L.h.mass[i] = 0;
+        }
+        __syncthreads();
+        const int shift = level == 0 ? 0 : max(0, 64 - __builtin_clzll((hi - lo) | 1ull) - 11);
+        const double top = level == 0 ? 0.0 : wt.exponent(ranking_score(hi));
+        auto scale_of = [&](int bin) { return level == 0 ? fmax((double)bin * (double)step * -wt.c, -1100.0) : top; };
+        // (an entry whose distance was rounded up into its bin may weigh a
+        // little more than the bin's scale: there is a bit of room for that)
+        auto value_bin = [&](float x, unsigned long long c) {
+            return level == 0 ? bin_of(x) : (int)((hi - c) >> shift);
+        };
+        each_four<THREADS>(row, N, [&](int64_t i, const float (&x)[4]) __attribute__((always_inline)) {
+#pragma unroll 1
+            for (int e = 0; e < 4; ++e) {
+                const float y = e == 0 ? x[0] : e == 1 ? x[1] : e == 2 ? x[2] : x[3];
+                if (!(y > -INFINITY)) continue;
+                const unsigned long long c = ranking(y, (uint32_t)(i + e));
+                if (c < lo || c > hi) continue;
+                const int bin = value_bin(y, c);
+                atomicAdd(&L.h.count[bin], 1u);
+                if (goal.by_mass)
+                    atomicAdd(&L.h.mass[bin],
+                              (unsigned long long)(pow2d(fmin(wt.exponent(y) - scale_of(bin), 0.5)) * unit));
+            }
+        });
+        __syncthreads();
+        find_bin(L, goal, [&](int bin) { return pow2d(scale_of(bin)) / unit; }, &count, &mass);
+        const int bin = L.bin;
+        const uint32_t in_bin = L.h.count[bin];
+        __syncthreads();
+        // the composites in that bin
+        if (tid == 0) {
+            L.lo = ~0ull;
+            L.hi = 0ull;
+            L.n = 0;
+        }
+        __syncthreads();
+        const bool take = in_bin <= (uint32_t)kSort;
+        unsigned long long mine_lo = ~0ull, mine_hi = 0ull;
+        each_four<THREADS>(row, N, [&](int64_t i, const float (&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!(x[e] > -INFINITY)) continue;
+                const unsigned long long c = ranking(x[e], (uint32_t)(i + e));
+                if (c < lo || c > hi || value_bin(x[e], c) != bin) continue;
+                mine_lo = min(mine_lo, c);
+                mine_hi = max(mine_hi, c);
+                if (take) L.s.c[atomicAdd(&L.n, 1u)] = c;
+            }
+        });
+        if (!take) {
+            if (mine_lo != ~0ull) {
+                atomicMin(&L.lo, mine_lo);
+                atomicMax(&L.hi, mine_hi);
+            }
+            __syncthreads();
+            lo = L.lo;
+            hi = L.hi;
+            __syncthreads();
+            continue;
+        }
+        __syncthreads();
+        const uint32_t at = sorted_cut(L, (int)in_bin, wt, goal, count, mass);
+        const uint64_t cut = L.s.c[at == in_bin ? in_bin - 1 : at];   // (short of the goal by rounding: the last one)
+        __syncthreads();
+        return cut;
+    }
 }
 
 // A double from another lane of the 16, by DPP (0 where there is none).
@@ -635,37 +661,49 @@ struct SamplePieces {
     int pieces;
 };
 
-template <typename T>
+// PER consecutive pieces per wavefront, the next one's scores loaded before the
+// sums of this one.
+template <typename T, int PER>
 __global__ __launch_bounds__(256) void k_sample_sums(SampleArgs a, SamplePieces q)
 {
     const int lane = threadIdx.x & 63;
     const int64_t b = blockIdx.x;
-    const int piece = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (piece >= q.pieces) return;
-    const int64_t wave = b * q.pieces + piece;
+    const int piece0 = (blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * PER;
+    if (piece0 >= q.pieces) return;
     const T* row = reinterpret_cast<const T*>(a.scores) + b * a.ld;
+    const double temperature = RowSettings(a, b).temperature;
     Four<T> f[4];
-    float x[4][4], best = -INFINITY;
+    auto load = [&](int piece) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j].load(row, (int64_t)piece * kPiece + j * 256 + lane * 4, a.N);
+        for (int j = 0; j < 4; ++j) f[j].load(row, (int64_t)piece * kPiece + j * 256 + lane * 4, a.N);
+    };
+    load(piece0);
+#pragma unroll 1
+    for (int k = 0; k < PER; ++k) {
+        const int piece = piece0 + k;
+        if (piece >= q.pieces) break;
+        float x[4][4], best = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j].get(x[j]);
-    if ((int64_t)(piece + 1) * kPiece > a.N) {
+        for (int j = 0; j < 4; ++j) f[j].get(x[j]);
+        if (PER > 1 && k + 1 < PER && piece + 1 < q.pieces) load(piece + 1);
+        if ((int64_t)(piece + 1) * kPiece > a.N) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) end4(x[j], (int64_t)piece * kPiece + j * 256 + lane * 4, a.N);
+            for (int j = 0; j < 4; ++j) end4(x[j], (int64_t)piece * kPiece + j * 256 + lane * 4, a.N);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) best = fmaxf(best, x[j][e]);
+        best = wave_reduce(best, OpMax());
+        const RowWeight wt(best, temperature);
+        const int64_t at = b * q.pieces + piece;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const double s = sum16((wt(x[j][0]) + wt(x[j][1])) + (wt(x[j][2]) + wt(x[j][3])));
+            if ((lane & (kRun - 1)) == 0) q.sums[at * 16 + j * 4 + lane / kRun] = s;
+        }
+        if (lane == 0) q.best[at] = best;
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) best = fmaxf(best, x[j][e]);
-    best = wave_reduce(best, OpMax());
-    const RowWeight wt(best, RowSettings(a, b).temperature);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const double s = sum16((wt(x[j][0]) + wt(x[j][1])) + (wt(x[j][2]) + wt(x[j][3])));
-        if ((lane & (kRun - 1)) == 0) q.sums[wave * 16 + j * 4 + lane / kRun] = s;
-    }
-    if (lane == 0) q.best[wave] = best;
 }
 
 template <typename T>
@@ -818,8 +856,8 @@ __device__ __forceinline__ void draw_kept(SampleLds<THREADS, CHUNKS>& L, const S
 // One workgroup per row. NV > 0: the row's scores in registers, NV vectors of
 // four a thread, element (j THREADS + thread) 4 + e; NV = 0: read again in each
 // pass.
-template <typename T, int THREADS, int NV, int CHUNKS>
-__global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
+template <typename T, int THREADS, int NV, int CHUNKS, int WAVES>
+__global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
 {
     constexpr int SW = THREADS / 64;
     __shared__ SampleLds<THREADS, CHUNKS> L;
@@ -867,19 +905,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
                 f((int64_t)(j * THREADS + tid) * 4, x);
             }
         } else {
-            // four vectors ahead
-            float x[4][4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) load4(row, (int64_t)(j * THREADS + tid) * 4, N, x[j]);
-#pragma unroll 1
-            for (int64_t i0 = 0; i0 < N; i0 += 4 * THREADS) {
-                f(i0 + tid * 4, x[0]);
-#pragma unroll
-                for (int j = 0; j < 3; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[j][e] = x[j + 1][e];
-                load4(row, i0 + (int64_t)(4 * THREADS + tid) * 4, N, x[3]);
-            }
+            each_four<THREADS>(row, N, f);
         }
     };
     float mine = -INFINITY;
@@ -1116,9 +1142,9 @@ __global__ __launch_bounds__(THREADS) void k_sample_rows(SampleArgs a)
 // equal scores around a cut than it sorts, a cut it did not find. One
 // workgroup per row, which is read once for each step of the search.
 template <typename T>
-__global__ __launch_bounds__(1024) void k_sample_far(SampleArgs a)
+__global__ __launch_bounds__(512) void k_sample_far(SampleArgs a)
 {
-    constexpr int THREADS = 1024, SW = THREADS / 64, CHUNKS = 4096;
+    constexpr int THREADS = 512, SW = THREADS / 64, CHUNKS = 4096;
     __shared__ SampleLds<THREADS, CHUNKS> L;
     const int tid = threadIdx.x;
     const int64_t b = blockIdx.x, N = a.N;
@@ -1126,11 +1152,13 @@ __global__ __launch_bounds__(1024) void k_sample_far(SampleArgs a)
     const T* row = reinterpret_cast<const T*>(a.scores) + b * a.ld;
     const RowSettings set(a, b);
     float M = -INFINITY, low = INFINITY;
-    for (int64_t i = tid; i < N; i += THREADS) {
-        const float x = row_value(row[i]);
-        M = fmaxf(M, x);
-        if (x > -INFINITY) low = fminf(low, x);
-    }
+    each_four<THREADS>(row, N, [&](int64_t, const float (&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            M = fmaxf(M, x[e]);
+            low = fminf(low, x[e] > -INFINITY ? x[e] : INFINITY);
+        }
+    });
     M = block_reduce<SW>(M, L.fbuf, OpMax());
     __syncthreads();
     low = -block_reduce<SW>(-low, L.fbuf, OpMax());
@@ -1145,10 +1173,10 @@ __global__ __launch_bounds__(1024) void k_sample_far(SampleArgs a)
         if (turn == 1) {
             // the weight that p is a share of
             double sum = 0.0;
-            for (int64_t i = tid; i < N; i += THREADS) {
-                const float x = row_value(row[i]);
-                if (x > -INFINITY && ranking(x, (uint32_t)i) >= cut) sum += wt(x);
-            }
+            each_four<THREADS>(row, N, [&](int64_t i, const float (&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += ranking(x[e], (uint32_t)(i + e)) >= cut ? wt(x[e]) : 0.0;
+            });
             sum = block_reduce<SW>(sum, L.dbuf, OpSum());
             __syncthreads();
             goal.mass = set.top_p * sum;
@@ -1161,16 +1189,31 @@ __global__ __launch_bounds__(1024) void k_sample_far(SampleArgs a)
     const int64_t len = 1ll << shift;
     const int n_chunks = (int)((N + len - 1) >> shift);
     __syncthreads();
-    for (int c = tid / 64; c < n_chunks; c += SW) {
+    auto four = [&](int64_t i, const float (&x)[4]) __attribute__((always_inline)) {
         double sum = 0.0;
-        const int64_t end = min(N, (c + 1) * len);
-        for (int64_t i = c * len + (tid & 63); i < end; i += 64) {
-            const float x = row_value(row[i]);
-            const double w = x > -INFINITY && ranking(x, (uint32_t)i) >= cut ? wt(x) : 0.0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const double w = ranking(x[e], (uint32_t)(i + e)) >= cut ? wt(x[e]) : 0.0;
             sum += w >= set.min_p ? w : 0.0;
         }
-        sum = wave_reduce(sum, OpSum());
-        if ((tid & 63) == 0) L.chunk[c] = sum;
+        return sum;
+    };
+    if (len == 64) {
+        each_four<THREADS>(row, N, [&](int64_t i, const float (&x)[4]) __attribute__((always_inline)) {
+            const double s = sum16(four(i, x));
+            if ((tid & (kRun - 1)) == 0 && i < N) L.chunk[i / 64] = s;
+        });
+    } else {
+        for (int c = tid / 64; c < n_chunks; c += SW) {
+            double s = 0.0;
+            for (int64_t i = c * len + (tid & 63) * 4; i < (c + 1) * len; i += 256) {
+                float x[4];
+                load4(row, i, N, x);
+                s += four(i, x);
+            }
+            s = wave_reduce(s, OpSum());
+            if ((tid & 63) == 0) L.chunk[c] = s;
+        }
     }
     draw_kept(L, a, b, row, wt, cut, set.min_p, n_chunks, len);
 }
@@ -1188,7 +1231,11 @@ void launch(const SampleArgs& a, hipStream_t s)
         const int pieces = (int)pieces_of(a.N);
         double* sums = reinterpret_cast<double*>(a.ws);
         const SamplePieces q{sums, reinterpret_cast<float*>(sums + (int64_t)a.batch * pieces * 16), pieces};
-        hipLaunchKernelGGL(k_sample_sums<T>, dim3(a.batch, (pieces + 3) / 4), dim3(256), 0, s, a, q);
+        // several pieces a wavefront where that leaves enough of them
+        if ((int64_t)a.batch * pieces >= 32768)
+            hipLaunchKernelGGL((k_sample_sums<T, 4>), dim3(a.batch, (pieces + 15) / 16), dim3(256), 0, s, a, q);
+        else
+            hipLaunchKernelGGL((k_sample_sums<T, 1>), dim3(a.batch, (pieces + 3) / 4), dim3(256), 0, s, a, q);
         hipLaunchKernelGGL(k_sample_draw<T>, dim3(a.batch), dim3(256), pieces * 16 * sizeof(double), s, a, q);
         return;
     }
@@ -1196,12 +1243,12 @@ void launch(const SampleArgs& a, hipStream_t s)
     // unit, the others one or two
     auto go = [&](auto kernel, int threads) {
         hipLaunchKernelGGL(kernel, dim3(a.batch), dim3(threads), 0, s, a);
-        hipLaunchKernelGGL(k_sample_far<T>, dim3(a.batch), dim3(1024), 0, s, a);
+        hipLaunchKernelGGL(k_sample_far<T>, dim3(a.batch), dim3(512), 0, s, a);
     };
-    if (a.N <= 4096) go(k_sample_rows<T, 256, 4, 64>, 256);
-    else if (a.N <= 16384) go(k_sample_rows<T, 1024, 4, 256>, 1024);
-    else if (a.N <= 65536) go(k_sample_rows<T, 512, 32, 1024>, 512);
-    else go(k_sample_rows<T, 1024, 0, 4096>, 1024);
+    if (a.N <= 4096) go(k_sample_rows<T, 256, 4, 64, 4>, 256);
+    else if (a.N <= 16384) go(k_sample_rows<T, 512, 8, 256, 4>, 512);
+    else if (a.N <= 65536) go(k_sample_rows<T, 512, 32, 1024, 2>, 512);
+    else go(k_sample_rows<T, 1024, 0, 4096, 4>, 1024);
 }
 
 }  // namespace
