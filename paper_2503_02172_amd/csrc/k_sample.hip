@@ -1060,8 +1060,18 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
     const int shift = chunk_shift<CHUNKS>(N);
     const int64_t len = 1ll << shift;
     const int n_chunks = (int)((N + len - 1) >> shift);
+    // Scores below `skip` have no part in it: those behind the cut, or without p
+    // those below min_p (a little lower, by what the logarithm and the sum round
+    // off); a wavefront without any other score goes on to its next ones.
+    float skip = cut ? ranking_score(cut) : -INFINITY;
+    if (!by_mass && min_p > 0.0) {
+        const double low = (double)M + set.temperature * (log(min_p) - 1e-6) - fabs((double)M) * 1e-6;
+        skip = fmaxf(skip, (float)fmax(low, -3e38));
+    }
     double z = 0.0, above = 0.0;
     auto four = [&](int64_t i, const float (&x)[4]) __attribute__((always_inline)) {
+        const bool none = !(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= skip);
+        if (__builtin_amdgcn_ballot_w64(!none) == 0) return 0.0;
         double w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = wt(x[e]);

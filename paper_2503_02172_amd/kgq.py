@@ -407,15 +407,16 @@ class Engine:
         if u.dim() != 2:
             raise ValueError("sample: u must be [B x S]")
         self._array("sample", "u", u, torch.float32, (B, u.shape[1]))
-        how = Sampling(1.0, 1.0, 0.0, 0)
-        kept = [scores, u]
-        for name, value in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
-            if torch.is_tensor(value):
+        rows, kept = {}, [scores, u]
+        settings = {"temperature": temperature, "top_k": top_k, "top_p": top_p, "min_p": min_p}
+        for name, value in settings.items():
+            if isinstance(value, torch.Tensor):
                 self._array("sample", name, value, torch.int32 if name == "top_k" else torch.float32, (B,))
-                setattr(how, name + "_rows", _ptr(value))
+                rows[name] = value.data_ptr()
+                settings[name] = 1                                 # (in every range; not used)
                 kept.append(value)
-            else:
-                setattr(how, name, value)
+        how = Sampling(settings["temperature"], settings["top_p"], settings["min_p"], settings["top_k"],
+                       rows.get("temperature"), rows.get("top_k"), rows.get("top_p"), rows.get("min_p"))
         need = ctypes.c_size_t()
         rc = lib().kgq_sample_workspace(self.h, B, ctypes.byref(need))
         if rc != OK:
