@@ -344,7 +344,8 @@ __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cu
     const T* g = reinterpret_cast<const T*>(a.grad) + col;
     O* out = reinterpret_cast<O*>(a.out) + col;
     uint32_t run = (uint32_t)keys[lo];
-    bool from_before = lo > 0 && (uint32_t)keys[lo - 1] == run;
+    const uint32_t ahead_of = (uint32_t)keys[max(lo - 1, 0)], behind = (uint32_t)keys[min(hi, a.n - 1)];
+    bool from_before = lo > 0 && ahead_of == run;
     float sum[V] = {};
     auto flush = [&](bool leaves) {
         if ((int64_t)run < a.rows) {
@@ -395,7 +396,7 @@ __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cu
             }
         }
     }
-    flush(hi < a.n && (uint32_t)keys[hi] == run);
+    flush(hi < a.n && behind == run);
 }
 
 // Pieces [lo, hi) of a run behind its first one, 256 columns: added to sum.
@@ -431,16 +432,20 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_grad_join(EmbedGradArgs a, 
     uint32_t run = 0;
     if (c + 1 < cut.chunks) {
         const int64_t next = (c + 1) * cut.chunk;    // (chunks but the last one are whole)
+        // (every key that the usual run asks for, in one go)
+        auto head = [&](int64_t k) { return (uint32_t)keys[min(k + lane, (int64_t)cut.chunks - 1) * cut.chunk]; };
         run = (uint32_t)keys[next - 1];
-        bool mine = (uint32_t)keys[next] == run && (int64_t)run < a.rows;
+        const uint32_t after = (uint32_t)keys[next], first = (uint32_t)keys[next - cut.chunk];
+        const uint32_t ahead = (uint32_t)keys[max(next - cut.chunk - 1, (int64_t)0)];
+        uint32_t heads = head(c + 1);
         // (not if it came from the chunk before)
-        if (mine && c > 0) mine = (uint32_t)keys[next - cut.chunk] != run || (uint32_t)keys[next - cut.chunk - 1] != run;
+        bool mine = after == run && (int64_t)run < a.rows && !(c > 0 && first == run && ahead == run);
         // the chunks behind c that begin with it, 64 at a look
-        for (int64_t k = c + 1; mine; k += 64) {
-            const uint64_t miss = __builtin_amdgcn_ballot_w64(!(k + lane < cut.chunks &&
-                                                                (uint32_t)keys[(k + lane) * cut.chunk] == run));
+        for (int64_t k = c + 1; mine; heads = head(k)) {
+            const uint64_t miss = __builtin_amdgcn_ballot_w64(!(k + lane < cut.chunks && heads == run));
             n += miss ? __builtin_ctzll(miss) : 64;
             mine = miss == 0;
+            k += 64;
         }
     }
     if (lane == 0) {

@@ -106,6 +106,19 @@ struct RowWeight {
     }
 };
 
+// A value that every lane holds, in scalar registers.
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x)
+{
+    // (the builtin returns an int: its sign must not spread over the upper half)
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32) |
+           (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x);
+}
+__device__ __forceinline__ double uniform(double x)
+{
+    return __builtin_bit_cast(double, uniform(__builtin_bit_cast(uint64_t, x)));
+}
+
 __device__ __forceinline__ uint64_t ranking(float x, uint32_t i)
 {
     return ((uint64_t)score_key(x) << 32) | (uint32_t)~i;
@@ -594,6 +607,7 @@ __device__ __forceinline__ int64_t pick_in(const T* row, int64_t N, const double
     bool back = false;
     for (int c = at;;) {
         if (c == n) {
+            if (at == 0) return -1;
             back = true;
             c = at - 1;
         }
@@ -837,7 +851,7 @@ __device__ __forceinline__ void draw_kept(SampleLds<THREADS, CHUNKS>& L, const S
         if (tid * per + j < n_chunks) L.chunk[tid * per + j] = run;
     }
     __syncthreads();
-    total = L.chunk[n_chunks - 1];
+    total = uniform(L.chunk[n_chunks - 1]);
     draw_all<THREADS>(L.d.share, L.d.idx, a, b, total, [&](double target, double* w) {
         return pick_in(row, N, L.chunk, n_chunks, len, target,
                       [&](const float (&x)[4], int64_t at, double (&v)[4]) {
@@ -915,7 +929,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
     } else {
         each([&](int64_t, const float (&x)[4]) { mine = fmaxf(mine, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))); });
     }
-    const float M = block_reduce<SW>(mine, L.fbuf, OpMax());
+    const float M = uniform(block_reduce<SW>(mine, L.fbuf, OpMax()));
     if (set.bad() || M == -INFINITY) {
         draw_nothing<THREADS>(a, b);
         return;
@@ -974,7 +988,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
             for (int e = 0; e < 4; ++e) low = fminf(low, x[e] > -INFINITY ? x[e] : M);
         });
         __syncthreads();
-        return -block_reduce<SW>(-low, L.fbuf, OpMax());
+        return uniform(-block_reduce<SW>(-low, L.fbuf, OpMax()));
     };
 
     if (set.top_k > 0 && set.top_k < N) {
@@ -983,7 +997,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
         float low = -INFINITY;
         if (set.top_k <= THREADS && N >= 4 * THREADS) {
             __syncthreads();
-            low = -block_reduce<SW>(-mine, L.fbuf, OpMax());
+            low = uniform(-block_reduce<SW>(-mine, L.fbuf, OpMax()));
         }
         if (low == -INFINITY) low = lowest();
         const CutGoal goal{false, (uint32_t)set.top_k, 0.0};
@@ -993,8 +1007,8 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
         uint32_t count = 0;
         double none = 0.0;
         find_bin(L, goal, [](int) { return 0.0; }, &count, &none);
-        const int bin = L.bin;
-        const uint32_t in_bin = L.h.count[bin];
+        const int bin = __builtin_amdgcn_readfirstlane(L.bin);
+        const uint32_t in_bin = __builtin_amdgcn_readfirstlane(L.h.count[bin]);
         if (in_bin > (uint32_t)kSort || goal.count > count + in_bin) return leave();
         if (tid == 0) L.n = 0;
         __syncthreads();
@@ -1006,7 +1020,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
         });
         __syncthreads();
         sort_list(L, (int)in_bin);
-        cut = L.s.c[goal.count - count - 1];
+        cut = uniform(L.s.c[goal.count - count - 1]);
         __syncthreads();
     }
 
@@ -1051,8 +1065,8 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
         for (int i = tid; i < CHUNKS; i += THREADS) L.s.extra[i] = 0ull;
         __syncthreads();
         if (L.bin == kBins || L.last == kBins) return leave();
-        from = (float)L.bin;
-        to = (float)(L.last + 1);
+        from = uniform((float)L.bin);
+        to = uniform((float)(L.last + 1));
     }
 
     // One pass in doubles: sums in index order, the total, and for top-p what
@@ -1124,15 +1138,15 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
         }
     }
     if (by_mass) {
-        z = block_reduce<SW>(z, L.dbuf, OpSum());
-        above = block_reduce<SW>(above, L.dbuf2, OpSum());
+        z = uniform(block_reduce<SW>(z, L.dbuf, OpSum()));
+        above = uniform(block_reduce<SW>(above, L.dbuf2, OpSum()));
         const CutGoal goal{true, 0u, p * z};
         const uint32_t n = L.n;
         __syncthreads();
         if (n == 0 || n > (uint32_t)kSort || !(above < goal.mass)) return leave();
         const uint32_t at = sorted_cut(L, (int)n, wt, goal, 0u, above);
         if (at == n) return leave();
-        cut = L.s.c[at];
+        cut = uniform(L.s.c[at]);
         // what is kept of the list goes to its chunks, in fixed point relative
         // to its largest weight
         const double top = wt(ranking_score(L.s.c[0])), unit = 0x1p50 / top;
