@@ -1083,9 +1083,11 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
         skip = fmaxf(skip, (float)fmax(low, -3e38));
     }
     double z = 0.0, above = 0.0;
-    auto four = [&](int64_t i, const float (&x)[4]) __attribute__((always_inline)) {
-        const bool none = !(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= skip);
-        if (__builtin_amdgcn_ballot_w64(!none) == 0) return 0.0;
+    // (whether the wavefront has anything to sum; sum: a lane's)
+    auto four = [&](int64_t i, const float (&x)[4], double& sum) __attribute__((always_inline)) {
+        sum = 0.0;
+        const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        if (__builtin_amdgcn_ballot_w64(top >= skip) == 0) return false;
         double w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = wt(x[e]);
@@ -1095,6 +1097,8 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
         }
         if (by_mass) {
             z += (w[0] + w[1]) + (w[2] + w[3]);
+            // all of it behind the bins?
+            if (__builtin_amdgcn_ballot_w64(bin_of(top) < to) == 0) return false;
             float v[4];
             bool in[4];
 #pragma unroll
@@ -1113,16 +1117,19 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = v[e] < from ? w[e] : 0.0;
         }
-        const double sum = (w[0] + w[1]) + (w[2] + w[3]);
+        sum = (w[0] + w[1]) + (w[2] + w[3]);
         above += sum;
-        if (!(min_p > 0.0)) return sum;
+        if (min_p > 0.0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = w[e] >= min_p ? w[e] : 0.0;
-        return (w[0] + w[1]) + (w[2] + w[3]);
+            for (int e = 0; e < 4; ++e) w[e] = w[e] >= min_p ? w[e] : 0.0;
+            sum = (w[0] + w[1]) + (w[2] + w[3]);
+        }
+        return true;
     };
     if (NV > 0 || len == 64) {
-        each([&](int64_t i, const float (&x)[4]) {
-            const double s = sum16(four(i, x));
+        each([&](int64_t i, const float (&x)[4]) __attribute__((always_inline)) {
+            double s;
+            if (four(i, x, s)) s = sum16(s);
             if ((tid & (kRun - 1)) == 0 && i < N) L.chunk[i / 64] = s;
         });
     } else {
@@ -1130,8 +1137,10 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
             double s = 0.0;
             for (int64_t i = c * len + (tid & 63) * 4; i < (c + 1) * len; i += 256) {
                 float x[4];
+                double part;
                 load4(row, i, N, x);
-                s += four(i, x);
+                four(i, x, part);
+                s += part;
             }
             s = wave_reduce(s, OpSum());
             if ((tid & 63) == 0) L.chunk[c] = s;
