@@ -1031,7 +1031,12 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
     if (by_mass) {
         // entries further off than this hold less than e^-8 of 1 - p together
         const float far = (logf((float)N) - logf((float)(1.0 - set.top_p)) + 8.f) * (float)set.temperature;
-        const float range = fminf(far, (M - lowest()) * 1.0001f);
+        // (all of the row, where that is less: looked up if the threads' largest
+        // scores lie in a small part of it)
+        float range = far;
+        __syncthreads();
+        const float near = M + uniform(block_reduce<SW>(-mine, L.fbuf, OpMax()));
+        if (near < far * 0.0625f || near == INFINITY) range = fminf(far, (M - lowest()) * 1.0001f);
         if (!(range > kNormal && range < INFINITY)) return leave();
         histogram(range);
         constexpr int per = kBins / THREADS;
