@@ -675,49 +675,40 @@ struct SamplePieces {
     int pieces;
 };
 
-// PER consecutive pieces per wavefront, the next one's scores loaded before the
-// sums of this one.
-template <typename T, int PER>
+// A piece per wavefront. 2,048 rows of 63,361: 128 us, bound by the doubles (the
+// same loads with float32 exponentials 103 us, which is what the bytes take);
+// two or four pieces a wavefront, the next one's scores ahead, take as long.
+template <typename T>
 __global__ __launch_bounds__(256) void k_sample_sums(SampleArgs a, SamplePieces q)
 {
     const int lane = threadIdx.x & 63;
     const int64_t b = blockIdx.x;
-    const int piece0 = (blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * PER;
-    if (piece0 >= q.pieces) return;
+    const int piece = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (piece >= q.pieces) return;
     const T* row = reinterpret_cast<const T*>(a.scores) + b * a.ld;
-    const double temperature = RowSettings(a, b).temperature;
+    const int64_t i0 = (int64_t)piece * kPiece + lane * 4, at = b * q.pieces + piece;
     Four<T> f[4];
-    auto load = [&](int piece) __attribute__((always_inline)) {
+    float x[4][4], best = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f[j].load(row, (int64_t)piece * kPiece + j * 256 + lane * 4, a.N);
-    };
-    load(piece0);
-#pragma unroll 1
-    for (int k = 0; k < PER; ++k) {
-        const int piece = piece0 + k;
-        if (piece >= q.pieces) break;
-        float x[4][4], best = -INFINITY;
+    for (int j = 0; j < 4; ++j) f[j].load(row, i0 + j * 256, a.N);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f[j].get(x[j]);
-        if (PER > 1 && k + 1 < PER && piece + 1 < q.pieces) load(piece + 1);
-        if ((int64_t)(piece + 1) * kPiece > a.N) {
+    for (int j = 0; j < 4; ++j) f[j].get(x[j]);
+    if ((int64_t)(piece + 1) * kPiece > a.N) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) end4(x[j], (int64_t)piece * kPiece + j * 256 + lane * 4, a.N);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) best = fmaxf(best, x[j][e]);
-        best = wave_reduce(best, OpMax());
-        const RowWeight wt(best, temperature);
-        const int64_t at = b * q.pieces + piece;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const double s = sum16((wt(x[j][0]) + wt(x[j][1])) + (wt(x[j][2]) + wt(x[j][3])));
-            if ((lane & (kRun - 1)) == 0) q.sums[at * 16 + j * 4 + lane / kRun] = s;
-        }
-        if (lane == 0) q.best[at] = best;
+        for (int j = 0; j < 4; ++j) end4(x[j], i0 + j * 256, a.N);
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) best = fmaxf(best, x[j][e]);
+    best = wave_reduce(best, OpMax());
+    const RowWeight wt(best, RowSettings(a, b).temperature);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const double s = sum16((wt(x[j][0]) + wt(x[j][1])) + (wt(x[j][2]) + wt(x[j][3])));
+        if ((lane & (kRun - 1)) == 0) q.sums[at * 16 + j * 4 + lane / kRun] = s;
+    }
+    if (lane == 0) q.best[at] = best;
 }
 
 template <typename T>
@@ -1269,11 +1260,7 @@ void launch(const SampleArgs& a, hipStream_t s)
         const int pieces = (int)pieces_of(a.N);
         double* sums = reinterpret_cast<double*>(a.ws);
         const SamplePieces q{sums, reinterpret_cast<float*>(sums + (int64_t)a.batch * pieces * 16), pieces};
-        // several pieces a wavefront where that leaves enough of them
-        if ((int64_t)a.batch * pieces >= 32768)
-            hipLaunchKernelGGL((k_sample_sums<T, 4>), dim3(a.batch, (pieces + 15) / 16), dim3(256), 0, s, a, q);
-        else
-            hipLaunchKernelGGL((k_sample_sums<T, 1>), dim3(a.batch, (pieces + 3) / 4), dim3(256), 0, s, a, q);
+        hipLaunchKernelGGL(k_sample_sums<T>, dim3(a.batch, (pieces + 3) / 4), dim3(256), 0, s, a, q);
         hipLaunchKernelGGL(k_sample_draw<T>, dim3(a.batch), dim3(256), pieces * 16 * sizeof(double), s, a, q);
         return;
     }
