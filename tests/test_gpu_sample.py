@@ -259,3 +259,44 @@ def test_gpu_sample_binding_refusals():
         eng.sample(x, u[:, :0].contiguous())
     with pytest.raises(kgq.KgqError):
         eng.sample(x.expand(2, 100)[:1].expand(2, 100), u)     # a row stride of 0
+
+
+@pytest.mark.parametrize("N", [262145, 327680, 327681, 500009])
+def test_gpu_sample_long_rows(N):
+    """Rows beyond what the running sums hold at 64 scores each, and beyond
+    those that are drawn from in pieces; with ties, which the first search
+    does not resolve."""
+    eng = engine(N)
+    x, u = scores(2, N, N), uniforms(2, 5, N + 1)
+    x[1] = np.random.default_rng(N).integers(-3, 3, N) / 4.0
+    for s in [dict(), dict(T=0.0), dict(k=50), dict(k=N - 1), dict(p=0.9), dict(m=0.05), dict(T=2.0, k=5000, p=0.95)]:
+        print(f"[sample] N={N} {s}", flush=True)
+        check(eng, x, u, f"N={N} {s}", **s)
+
+
+@pytest.mark.parametrize("N", [300, 70000])
+def test_gpu_sample_more_draws_than_are_taken_together(N):
+    eng = engine(N)
+    x, u = scores(2, N, 5), uniforms(2, 2500, 6)
+    for s in [dict(), dict(p=0.8), dict(k=20)]:
+        check(eng, x, u, f"N={N} {s}", **s)
+
+
+def test_gpu_sample_calls_that_overlap():
+    """Calls on four streams at once, each with its own workspace, give what
+    they give alone; one handle in checked mode among them."""
+    import torch
+    N, B = 30011, 40
+    eng, checked = engine(N), engine(N)
+    checked.set_checked(True)
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    u = torch.as_tensor(uniforms(B, 16, 1), device="cuda")
+    args = [(e, torch.as_tensor(scores(B, N, 80 + i), device="cuda"), kw) for i, (e, kw) in
+            enumerate(((eng, dict()), (eng, dict(top_p=0.9)), (checked, dict()), (eng, dict(top_k=77))))]
+    alone = [e.sample(t, u, **kw) for e, t, kw in args]
+    torch.cuda.synchronize()
+    outs = [[e.sample(t, u, stream=s, **kw) for s, (e, t, kw) in zip(streams, args)] for _ in range(5)]
+    torch.cuda.synchronize()
+    for turn in outs:
+        for got, want in zip(turn, alone):
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
