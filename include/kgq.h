@@ -588,7 +588,8 @@ kgq_status kgq_embed(kgq_handle* h, const void* table, int32_t dtype, int64_t ro
  *               of range add nothing
  *   out         device [rows x dim] of out_dtype, row stride ld_out. accumulate
  *               0: every row is written, zeros where no token has its id;
- *               otherwise rows without a token are left as they are
+ *               otherwise rows without a token are left as they are. Must not
+ *               overlap grad
  *   ws          device memory, 16-byte aligned, of at least the bytes that
  *               kgq_embed_grad_workspace reports; a call owns it until it has
  *               run, so calls that may overlap need one each

@@ -112,7 +112,8 @@ void launch_embed(const EmbedArgs& a, hipStream_t s)
     // four vectors a thread where that still leaves two workgroups a compute
     // unit; one where latency counts
     const bool many = (int64_t)a.n * vecs >= (int64_t)512 * 1024;
-    const int per = std::max(1, (many ? 1024 : 256) / vecs);
+    // (a launch has fewer than 2^32 threads)
+    const int per = std::max({1, (many ? 1024 : 256) / vecs, (int)(((int64_t)a.n + (1 << 23) - 1) >> 23)});
     const uint32_t inv = (uint32_t)(((1ull << 32) + vecs - 1) / vecs);
     const dim3 grid((uint32_t)(((int64_t)a.n + per - 1) / per));
     if (many) hipLaunchKernelGGL((k_embed_rows<T, O, 4>), grid, dim3(256), 0, s, a, per, vecs, inv);
@@ -362,30 +363,31 @@ __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cu
     // a whole wavefront per group: its chunk's keys and tokens in one load, then
     // from lane to scalar register
     uint32_t keys_ahead = 0, tokens_ahead = 0;
-    if (WIDE && lo + (int)(threadIdx.x & 63) < hi) {
+    const int count = hi - lo;                       // (positions are counted from lo: hi may be the largest int)
+    if (WIDE && (int)(threadIdx.x & 63) < count) {
         keys_ahead = (uint32_t)keys[lo + (threadIdx.x & 63)];
         tokens_ahead = (uint32_t)tokens[lo + (threadIdx.x & 63)];
     }
-    for (int i0 = lo; i0 < hi; i0 += kAhead) {
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
         float x[kAhead][V];
         uint32_t key[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int i = min(i0 + u, hi - 1);
+            const int i = min(i0 + u, count - 1);
             int64_t token;
             if (WIDE) {
-                key[u] = __builtin_amdgcn_readlane(keys_ahead, i - lo);
-                token = __builtin_amdgcn_readlane(tokens_ahead, i - lo);
+                key[u] = __builtin_amdgcn_readlane(keys_ahead, i);
+                token = __builtin_amdgcn_readlane(tokens_ahead, i);
             } else {
-                key[u] = (uint32_t)keys[i];
-                token = tokens[i];
+                key[u] = (uint32_t)keys[lo + i];
+                token = tokens[lo + i];
             }
             // (rows of tokens without an id are not read)
             if ((int64_t)key[u] < a.rows) load_columns<V>(g + token * a.ld, left, x[u]);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (i0 + u >= hi) break;
+            if (i0 + u >= count) break;
             if (key[u] != run) {
                 flush(false);
                 run = key[u];

@@ -268,3 +268,58 @@ def test_gpu_a_students_step():
         mine = (host(dE) * vE).sum() + (host(dR) * vR).sum()
         # products of 32 to 700 float32 terms, 24 bits each
         assert abs(diff - mine) < 1e-4 * (np.abs(host(dE) * vE).sum() + np.abs(host(dR) * vR).sum())
+
+
+def test_gpu_embed_more_tokens_than_workgroups(eng):
+    """Rows long enough for a workgroup each, and more of them than a launch
+    can have workgroups of 256 threads."""
+    import torch
+    n, d = (1 << 24) + 3, 2049
+    if torch.cuda.mem_get_info()[0] < 90e9:
+        pytest.skip("needs 69 GB of device memory")
+    t = torch.randn(3, d, device="cuda")
+    ids = torch.arange(n, dtype=torch.int32, device="cuda") % 4 - 1
+    got = eng.embed(t, ids, dtype=torch.bfloat16)
+    for at in (0, 1, 2, 3, 4, (1 << 23) - 1, 1 << 23, (1 << 24) - 1, 1 << 24, n - 2, n - 1):
+        want = t[at % 4 - 1].bfloat16() if at % 4 else torch.zeros(d, device="cuda").bfloat16()
+        assert torch.equal(got[at], want), at
+    del got
+    torch.cuda.empty_cache()
+
+
+def test_gpu_embed_grad_calls_that_overlap(eng):
+    """Calls on four streams at once, each with its own workspace, give what
+    they give alone."""
+    import torch
+    V, d = 20000, 96
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    args = [(dev(ids_of(n, V, 70 + n), None), torch.randn(n, d, device="cuda")) for n in (50000, 3000, 50001, 4097)]
+    alone = [eng.embed_grad(g, ids, V) for ids, g in args]
+    torch.cuda.synchronize()
+    outs = [[eng.embed_grad(g, ids, V, stream=s) for s, (ids, g) in zip(streams, args)] for _ in range(5)]
+    torch.cuda.synchronize()
+    for turn in outs:
+        for got, want in zip(turn, alone):
+            assert torch.equal(got, want)
+
+
+def test_gpu_embed_grad_one_id_and_padding_alone(eng):
+    """Every token the same id (one run over all chunks), the last id of the
+    table, and a batch of padding alone: rows without a token are zeros, or
+    stay as they are."""
+    import torch
+    for n, d in ((4097, 8), (4096, 300), (100000, 3), (200, 2000)):
+        V = 300
+        g = torch.randn(n, d, device="cuda")
+        ids = torch.full((n,), V - 1, dtype=torch.int32, device="cuda")
+        got = eng.embed_grad(g, ids, V)
+        want = g.double().sum(0)
+        # n additions in float32, each off by at most 2^-24 of the sum of the magnitudes
+        bound = 2.0 ** -24 * n * g.abs().double().sum(0).max()
+        assert (got[V - 1].double() - want).abs().max() <= bound
+        assert not got[:V - 1].any()
+        pad = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+        old = torch.randn(V, d, device="cuda")
+        kept = eng.embed_grad(g, pad, V, out=old.clone(), accumulate=True)
+        assert torch.equal(kept, old)
+        assert not eng.embed_grad(g, pad, V).any()
