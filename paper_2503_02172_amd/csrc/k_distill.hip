@@ -68,6 +68,12 @@ __device__ __forceinline__ float word_value(const W& w, int e)
 // scores' place, or (KEEP false, bfloat16: half the registers, and twice the
 // rows in flight) are computed again for the gradient. NV = 0: the row is read
 // twice. Three barriers: behind the maxima, the sums, and the row's stores.
+// Bound by memory where rows are many: 2,048 rows of 63,361, K = 100: 237 us,
+// 4.4 TB/s read and written (a plain copy of the scores 195 us: it has no
+// barrier between its loads and its stores, and more than one row a compute
+// unit to fill the gaps). 1,024 in bfloat16, K = 1,000: 98 us, 2.6 TB/s, where
+// the exponentials, two a score, take as long as the bytes. 509 rows of 14,505:
+// 15.7 us, 3.8 TB/s. 32 rows of 1,000: 6 us, the latency of the three barriers.
 template <typename T, int DT, int NV, bool KEEP, int WAVES>
 __global__ __launch_bounds__(DT, WAVES) void k_distill(DistillArgs a, float chi, float clo, int slots)
 {
@@ -340,14 +346,25 @@ void launch(const DistillArgs& a, hipStream_t s)
     auto go = [&](auto kernel, int threads) {
         hipLaunchKernelGGL(kernel, dim3(a.batch), dim3(threads), 0, s, a, chi, clo, slots);
     };
-    // the row in registers where it fits: 16 or 32 scores a thread up to 16,384,
-    // which leaves several rows to a compute unit; 128 up to 65,536, one row a
-    // compute unit (bfloat16: two)
-    constexpr bool half = sizeof(T) == 2;
-    if (a.N <= 4096) go(k_distill<T, 256, 16 / V, true, 4>, 256);
-    else if (a.N <= 16384) go(k_distill<T, 512, 32 / V, true, 4>, 512);
-    else if (a.N <= 65536) go(k_distill<T, 512, 128 / V, !half, half ? 4 : 2>, 512);
-    else go(k_distill<T, 1024, 0, false, 4>, 1024);
+    // The row in registers where it fits, several rows to a compute unit where
+    // the scores are few: 16 a thread up to 4,096 (2,048 rows of 4,000: 21 us, 35
+    // with 32 a thread), 32 up to 16,384 (of 14,505: 45 us, 109 with 128), 128 up
+    // to 65,536 (of 63,361: 237 us, 327 read twice; one row: 15 and 22). Of
+    // bfloat16, two rows fit a compute unit if the exponentials are computed
+    // twice: slower up to two rows a compute unit (one row 20 us, 15 kept; 512:
+    // 42 and 41), faster behind (2,048: 152 and 176).
+    if (a.N <= 4096) {
+        go(k_distill<T, 256, 16 / V, true, 4>, 256);
+    } else if (a.N <= 16384) {
+        go(k_distill<T, 512, 32 / V, true, 4>, 512);
+    } else if (a.N <= 65536) {
+        if constexpr (sizeof(T) == 2) {
+            if (a.batch > 512) return go(k_distill<T, 512, 128 / V, false, 4>, 512);
+        }
+        go(k_distill<T, 512, 128 / V, true, 2>, 512);
+    } else {
+        go(k_distill<T, 1024, 0, false, 4>, 1024);
+    }
 }
 
 }  // namespace
