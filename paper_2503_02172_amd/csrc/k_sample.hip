@@ -38,7 +38,7 @@ namespace {
 
 constexpr int kBins = 2048;
 constexpr int kSort = 2048;                  // entries that are sorted for a cut
-constexpr int kRankSort = 512;               // of these, sorted by counting
+constexpr int kRankSort = 512;               // of these, sorted by counting (top-p, 2,048 rows: 379 us, 404 by merging)
 constexpr int kDrawn = 1024;                 // draws of a row whose logarithms are taken together
 constexpr int kRun = 16;                     // lanes per draw, and per 64 scores
 constexpr int kPiece = 1024;                 // scores of a row per wavefront, without cuts
@@ -72,8 +72,8 @@ __device__ __forceinline__ double pow2d(double t)
 // weight. Rounding and scaling by n take an addition each instead of the
 // instructions of that name, which run at a quarter of the rate or less: the
 // sum of 1.5 2^52 and a number holds it rounded in its low bits, and adding n to
-// the exponent field multiplies by 2^n. (The sums of 2,048 rows of 63,361: 132
-// us with those instructions.)
+// the exponent field multiplies by 2^n. (The sums of 2,048 rows of 63,361 take
+// 144 us with those instructions, 128 without.)
 struct RowWeight {
     float top, low, from;                    // scores are taken into [low, top]; below `from` they have no weight
     double M, c;
@@ -711,6 +711,11 @@ __global__ __launch_bounds__(256) void k_sample_sums(SampleArgs a, SamplePieces 
     if (lane == 0) q.best[at] = best;
 }
 
+// A row's draws from its pieces' sums: a workgroup per row, as many as fit a
+// compute unit. 2,048 rows of 63,361, 128 draws each: 56 us, bound by issue (64
+// weights in doubles a draw; 64 us with slower ones) and by the three lines of
+// 128 bytes that a draw's 64 scores touch, 100 MB; four draws ahead a group, or
+// more wavefronts at the price of registers, are no faster (56 to 99 us).
 template <typename T>
 __global__ __launch_bounds__(256) void k_sample_draw(SampleArgs a, SamplePieces q)
 {
@@ -861,6 +866,14 @@ __device__ __forceinline__ void draw_kept(SampleLds<THREADS, CHUNKS>& L, const S
 // One workgroup per row. NV > 0: the row's scores in registers, NV vectors of
 // four a thread, element (j THREADS + thread) 4 + e; NV = 0: read again in each
 // pass.
+// 2,048 rows of 63,361, top-p 0.9: 388 us, 1.3 TB/s. A row takes about 42 us of
+// its compute unit, one row after the other: loading 6, largest score 1,
+// histogram 7, its bins 2, the pass in doubles 18, list and cut 3, the draw
+// 3.5. So the phases' latency bounds it, and the doubles, which cost 18 us a row
+// here and bound the sums without cuts at 16. (256 of the 512 registers of a
+// lane hold scores: a second row does not fit; 1,024 threads with half as many
+// each spill.) top-k 100: 284 us, min-p 160. 61 rows with all cuts: 59 us, and
+// one row of 14,505 with top-p 20: the latency of the phases alone.
 template <typename T, int THREADS, int NV, int CHUNKS, int WAVES>
 __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
 {
@@ -1169,7 +1182,8 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
 
 // The rows that k_sample_rows left: infinite scores, more equal or nearly
 // equal scores around a cut than it sorts, a cut it did not find. One
-// workgroup per row, which is read once for each step of the search.
+// workgroup per row, which is read once for each step of the search. 4 us where
+// there is no such row.
 template <typename T>
 __global__ __launch_bounds__(512) void k_sample_far(SampleArgs a)
 {
@@ -1256,6 +1270,8 @@ void launch(const SampleArgs& a, hipStream_t s)
 {
     const bool cuts = a.top_k_rows || a.top_p_rows || a.min_p_rows || (a.top_k > 0 && a.top_k < a.N) || a.top_p < 1.0 ||
                       a.min_p > 0.0;
+    // (2,048 rows of 63,361 without cuts, 4 draws each: 142 us so, 246 by
+    // k_sample_rows; of 1,000: 17 and 24; one row of 63,361: 11 and 26)
     if (!cuts && pieces_of(a.N) <= kMaxPieces) {
         const int pieces = (int)pieces_of(a.N);
         double* sums = reinterpret_cast<double*>(a.ws);
@@ -1264,13 +1280,19 @@ void launch(const SampleArgs& a, hipStream_t s)
         hipLaunchKernelGGL(k_sample_draw<T>, dim3(a.batch), dim3(256), pieces * 16 * sizeof(double), s, a, q);
         return;
     }
-    // the row in registers where it fits; short rows four or more to a compute
-    // unit, the others one or two
+    // The row in registers where it fits: 16 scores a thread of 256 up to 4,096
+    // (top-p, 2,048 rows of 4,000: 47 us, 104 with 32 a thread of 512; one row:
+    // 16 and 23); up to 16,384, 16 of 1,024 where every row has a compute unit
+    // (one row of 14,505: 22 us, top-k 19; with 32 of 512 23.5 and 24), else 32 of
+    // 512, two or more rows to a unit (2,048 rows: 115 us, 165 and with 128 of
+    // 512 304); 128 of 512 up to 65,536 (of 63,361: 379 us, 467 read again in each
+    // pass; one row: 37 and 44).
     auto go = [&](auto kernel, int threads) {
         hipLaunchKernelGGL(kernel, dim3(a.batch), dim3(threads), 0, s, a);
         hipLaunchKernelGGL(k_sample_far<T>, dim3(a.batch), dim3(512), 0, s, a);
     };
     if (a.N <= 4096) go(k_sample_rows<T, 256, 4, 64, 4>, 256);
+    else if (a.N <= 16384 && a.batch <= 256) go(k_sample_rows<T, 1024, 4, 256, 4>, 1024);
     else if (a.N <= 16384) go(k_sample_rows<T, 512, 8, 256, 4>, 512);
     else if (a.N <= 65536) go(k_sample_rows<T, 512, 32, 1024, 2>, 512);
     else go(k_sample_rows<T, 1024, 0, 4096, 4>, 1024);

@@ -240,3 +240,17 @@ def test_gpu_distill_binding_refusals():
     for kw in (dict(temperature=0.0), dict(temperature=float("nan")), dict(loss=False, grad=False)):
         with pytest.raises(kgq.KgqError):
             eng.distill(s, idx, t, **kw)
+
+
+@pytest.mark.parametrize("N", [4096, 16384, 16385, 65536])
+def test_gpu_distill_many_bfloat16_rows(N):
+    """Rows at the ends of what a workgroup holds, few and more than two to a
+    compute unit."""
+    eng = engine(N)
+    for B in (2, 530):
+        z, idx, t, w = inputs(B, N, 50, 7)
+        z[0, N // 2:] = -np.inf
+        a = check(eng, z, idx, t, 2.0, w, f"B={B}", dtype="bf16")
+        b = check(eng, z, idx, t, 2.0, w, f"B={B}, in place", dtype="bf16", pad=5, out="scores")
+        np.testing.assert_array_equal(a[0], b[0])
+        np.testing.assert_array_equal(a[1], b[1])

@@ -300,3 +300,16 @@ def test_gpu_sample_calls_that_overlap():
     for turn in outs:
         for got, want in zip(turn, alone):
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("N", [4096, 4097, 9001, 16384, 16385, 65536])
+def test_gpu_sample_few_and_many_rows(N):
+    """Rows at the ends of what a workgroup holds, few and more than one to a
+    compute unit."""
+    eng = engine(N)
+    for B in (2, 259):
+        x, u = scores(B, N, N + B), uniforms(B, 3, N)
+        x[0] = np.random.default_rng(N).integers(-3, 3, N) / 4.0
+        x[1, N // 2:] = -np.inf
+        for s in [dict(), dict(k=50), dict(p=0.9), dict(T=2.0, k=1000, p=0.95, m=0.01)]:
+            check(eng, x, u, f"N={N} B={B} {s}", **s)
