@@ -575,7 +575,7 @@ kgq_status kgq_distill(kgq_handle* h, int32_t batch, const void* scores, int32_t
  * The product is float32, rounded once for a bfloat16 output. n = 0 does
  * nothing.
  * Errors: INVALID_ARG (NULL pointers, unknown dtypes, rows outside [1, 2^31-1],
- * dim < 1, n < 0, a stride below dim; checked mode under capture),
+ * dim outside [1, 2^24], n < 0, a stride below dim; checked mode under capture),
  * OUT_OF_RANGE (checked), NO_DEVICE, DEVICE. */
 kgq_status kgq_embed(kgq_handle* h, const void* table, int32_t dtype, int64_t rows, int32_t dim, int64_t ld,
                      const int32_t* ids, int32_t n, float scale, void* out, int32_t out_dtype, int64_t ld_out,

@@ -8,7 +8,8 @@
 // whatever their ids, so that an id with many tokens is summed by many
 // wavefronts: a run of one id that lies inside a chunk goes to the table, a
 // piece of a run that continues in another chunk to the workspace, and a last
-// launch adds such pieces in chunk order.
+// launch adds such pieces in chunk order. Few tokens take one launch, which
+// compares their ids instead of sorting them.
 #include <algorithm>
 
 #include "row_ops.hpp"
@@ -20,7 +21,10 @@ namespace {
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortBlocks = 128;             // blocks of a pass at most
-constexpr int kSortShort = 4096;             // tokens that the counting sort takes
+constexpr int kFew = 2048;                   // tokens whose gradient takes one launch
+constexpr int kFewWaves = 8;
+constexpr int kFewAlone = 9;                 // tokens of an id that one wavefront adds
+constexpr int kFewSplit = 64;                // workgroups of a token at most
 constexpr int kJoinWaves = 16;
 constexpr int kJoinAhead = 16;               // pieces in flight per wavefront
 constexpr int kJoinAlone = 32;               // pieces of a run that one wavefront adds
@@ -134,6 +138,131 @@ void launch_embed_rows(const EmbedArgs& a, hipStream_t s)
     else launch_embed<uint16_t, uint16_t>(a, s);
 }
 
+// ---- gradient of few tokens ---------------------------------------------------
+
+// One launch. A workgroup takes a token and some blocks of 64 x 16 bytes of
+// columns: it looks through all ids for its own, leaves it to the token before
+// if there is one with the same id, and otherwise adds the rows of all of them
+// in token order. Up to kFewAlone of them, a wavefront adds all of a block; more,
+// each adds a share of them, and the shares are added in order. The workgroups
+// behind the tokens' write zeros to the rows whose number they do not find among
+// the ids. 1,536 tokens of 400 to 14,505 rows: 10.6 us (10 without the zeros' 23
+// MB), the latency of a launch, the ids, the rows and one exchange. As many
+// wavefronts as keep the hottest ids short: with four 15.3 us, with 16 16.8.
+template <typename T, typename O>
+__global__ __launch_bounds__(64 * kFewWaves) void k_grad_few(EmbedGradArgs a, int blocks, int split)
+{
+    constexpr int V = RowVec<T>::n, AHEAD = 32 / V, THREADS = 64 * kFewWaves;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int token_groups = a.n * split;
+    if ((int)blockIdx.x >= token_groups) {
+        constexpr int VO = RowVec<O>::n, PER = 64, ROWS = PER / kFewWaves;
+        __shared__ unsigned long long used;
+        const int64_t step = (int64_t)(gridDim.x - token_groups) * PER;
+        for (int64_t v0 = (int64_t)(blockIdx.x - token_groups) * PER; v0 < a.rows; v0 += step) {
+            __syncthreads();
+            if (tid == 0) used = 0ull;
+            __syncthreads();
+            for (int i = tid; i < a.n; i += THREADS) {
+                const int64_t at = a.ids[i] - v0;
+                if (at >= 0 && at < PER) atomicOr(&used, 1ull << at);
+            }
+            __syncthreads();
+            const uint64_t mine = used >> (wave * ROWS);
+            for (int r = 0; r < ROWS; ++r) {
+                const int64_t v = v0 + wave * ROWS + r;
+                if (v >= a.rows) break;
+                if (mine >> r & 1) continue;
+                const float zero[VO] = {};
+                for (int c = lane * VO; c < a.d; c += 64 * VO)
+                    store_columns<VO, true>(reinterpret_cast<O*>(a.out) + v * a.ld_out + c, a.d - c, zero, 1.f, false);
+            }
+        }
+        return;
+    }
+    __shared__ uint64_t same[kFew / 64];             // the tokens with this id, as bits
+    __shared__ uint16_t list[kFew];                  // and as a list
+    __shared__ float share[kFewWaves][64 * V];
+    const int t = blockIdx.x / split, block0 = blockIdx.x % split;   // (blocks block0, block0 + split, ...)
+    const int32_t id = a.ids[t];
+    if (id < 0 || id >= a.rows) {
+        if (id != -1 && a.flag && tid == 0) atomicOr(a.flag, kErrRange);
+        return;
+    }
+    const T* g = reinterpret_cast<const T*>(a.grad);
+    O* out = reinterpret_cast<O*>(a.out) + (int64_t)id * a.ld_out;
+    // (the token's own row meanwhile)
+    int col = ((block0 + wave * split) * 64 + lane) * V;
+    float sum[V];
+    load_columns<V>(g + t * a.ld + col, a.d - col, sum);
+    const int words = (a.n + 63) / 64;
+    for (int w = wave; w < words; w += kFewWaves) {
+        const int i = w * 64 + lane;
+        const uint64_t m = __builtin_amdgcn_ballot_w64(i < a.n && a.ids[min(i, a.n - 1)] == id);
+        if (lane == 0) same[w] = m;
+    }
+    __syncthreads();
+    const uint64_t m = lane < words ? same[lane] : 0ull;
+    const uint64_t before_t = lane < t / 64 ? m : lane == t / 64 ? m & ((1ull << (t & 63)) - 1) : 0ull;
+    if (__builtin_amdgcn_ballot_w64(before_t != 0)) return;
+    int upto = __popcll(m);                          // running count of the tokens in the words up to this lane's
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(upto, d, 64);
+        if (lane >= d) upto += o;
+    }
+    const int total = __builtin_amdgcn_readlane(upto, 63);
+    if (total > 1) {
+        const int from = upto - __popcll(m);
+        for (int w = wave; w < words; w += kFewWaves) {
+            const uint64_t mw = same[w];
+            const int at = __shfl(from, w, 64) + __popcll(mw & ((1ull << lane) - 1));
+            if (mw >> lane & 1) list[at] = (uint16_t)(w * 64 + lane);
+        }
+        __syncthreads();
+    }
+    auto add = [&](int lo, int hi) __attribute__((always_inline)) {
+        for (int i0 = lo; i0 < hi; i0 += AHEAD) {
+            float x[AHEAD][V];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t token = __builtin_amdgcn_readfirstlane((int)list[min(i0 + u, hi - 1)]);
+                load_columns<V>(g + token * a.ld + col, a.d - col, x[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += i0 + u < hi ? x[u][j] : 0.f;
+        }
+    };
+    if (total <= kFewAlone) {
+        for (int k = wave; block0 + k * split < blocks; k += kFewWaves) {
+            col = ((block0 + k * split) * 64 + lane) * V;
+            if (k != wave) load_columns<V>(g + t * a.ld + col, a.d - col, sum);
+            add(1, total);
+            store_columns<V, true>(out + col, a.d - col, sum, a.scale, a.accumulate != 0);
+        }
+        return;
+    }
+    const int per = (total + kFewWaves - 1) / kFewWaves, lo = min(total, wave * per), hi = min(total, lo + per);
+    for (int block = block0; block < blocks; block += split) {
+        col = (block * 64 + lane) * V;
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] = 0.f;
+        add(lo, hi);
+#pragma unroll
+        for (int j = 0; j < V; ++j) share[wave][lane * V + j] = sum[j];
+        __syncthreads();
+        if (wave == 0) {
+            for (int w = 1; w < kFewWaves; ++w)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += share[w][lane * V + j];
+            store_columns<V, true>(out + col, a.d - col, sum, a.scale, a.accumulate != 0);
+        }
+        __syncthreads();
+    }
+}
+
 // ---- tokens sorted by id ----------------------------------------------------
 
 // A token's key: its id, or `rows` (behind every row) for what is no row.
@@ -145,42 +274,7 @@ __device__ __forceinline__ uint32_t token_key(const EmbedGradArgs& a, int64_t i)
     return (uint32_t)a.rows;
 }
 
-// Few tokens: a token's place is the number of tokens with a smaller key, or
-// the same key and earlier. One launch; n^2 comparisons, spread over the chip
-// (64 tokens per workgroup, each of 16 wavefronts against its share of all).
-// 1,536 tokens: 6 us, a launch and the keys' way to LDS. Up to kSortShort tokens:
-// the whole gradient of 1,536 tokens of 400 takes 22 us so and 29 by digits, of
-// 4,096 29.5 and 30.6.
-__global__ __launch_bounds__(kSortThreads) void k_sort_short(EmbedGradArgs a, int32_t* keys_out, int32_t* tokens_out)
-{
-    __shared__ alignas(16) uint32_t key[kSortShort];
-    __shared__ uint32_t before[kSortWaves][64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int padded = (a.n + 4 * kSortWaves - 1) / (4 * kSortWaves) * (4 * kSortWaves);
-    for (int i = tid; i < padded; i += kSortThreads) key[i] = i < a.n ? token_key(a, i) : ~0u;
-    __syncthreads();
-    const int t = blockIdx.x * 64 + lane;
-    const uint32_t mine = t < a.n ? key[t] : 0u;
-    uint32_t count = 0;
-    const int part = padded / kSortWaves, lo = wave * part;
-#pragma unroll 4
-    for (int j = lo; j < lo + part; j += 4) {
-        const uint4 k = *reinterpret_cast<const uint4*>(&key[j]);
-        count += (k.x < mine + (j < t)) + (k.y < mine + (j + 1 < t)) + (k.z < mine + (j + 2 < t)) +
-                 (k.w < mine + (j + 3 < t));
-    }
-    before[wave][lane] = count;
-    __syncthreads();
-    if (wave == 0 && t < a.n) {
-        uint32_t at = 0;
-#pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) at += before[w][lane];
-        keys_out[at] = (int32_t)mine;
-        tokens_out[at] = t;
-    }
-}
-
-// Many tokens: least significant digit first, 8 bits a pass, two launches a
+// Least significant digit first, 8 bits a pass, two launches a
 // pass. Block b takes the positions [b * span, (b + 1) * span) tile by tile
 // (one position per thread); hist[b * 256 + digit] is the number of its keys
 // with that digit. The first pass reads the ids themselves. 262,144 tokens: 4.7
@@ -562,39 +656,59 @@ int64_t embed_grad_workspace(int64_t n, int d)
     return 4 * align256(n * 4) + align256((int64_t)256 * sort_blocks(n) * 4) + align256(2 * pieces * d * 4);
 }
 
-void launch_embed_grad(const EmbedGradArgs& a, hipStream_t s)
+namespace {
+
+template <typename T, typename O>
+void launch_all(const EmbedGradArgs& a, hipStream_t s)
 {
+    // One launch instead of six or more: 12 us for 1,536 tokens of 400 and 29
+    // sorted, 61: 8 and 23, 2,500: 17 and 30, 4,096: 26 and 31. But ids with
+    // hundreds of tokens take longer than sorted (1,536 of one id: 57 us and 30),
+    // and longer the more tokens: hence no more than kFew.
+    if (a.n <= kFew) {
+        const int blocks = (a.d + 64 * RowVec<T>::n - 1) / (64 * RowVec<T>::n);
+        const int64_t fill = a.accumulate ? 0 : std::min<int64_t>((a.rows + 63) / 64, 1 << 18);
+        // two blocks of columns a workgroup: an id with every token of 2,048 of
+        // 2,000 columns takes 94 us so, 302 with all in one (no two alike: 47, 32)
+        const int split = std::min((blocks + 1) / 2, kFewSplit);
+        if (a.n + fill > 0)
+            hipLaunchKernelGGL((k_grad_few<T, O>), dim3((uint32_t)(a.n * split + fill)), dim3(64 * kFewWaves), 0, s, a,
+                               blocks, split);
+        return;
+    }
     char* ws = reinterpret_cast<char*>(a.ws);
     int32_t* buf[4];
     for (auto& b : buf) {
         b = reinterpret_cast<int32_t*>(ws);
         ws += align256((int64_t)a.n * 4);
     }
-    const int blocks = sort_blocks(a.n);
+    const int sorters = sort_blocks(a.n);
     uint32_t* hist = reinterpret_cast<uint32_t*>(ws);
-    float* piece = reinterpret_cast<float*>(ws + align256((int64_t)256 * blocks * 4));
+    float* piece = reinterpret_cast<float*>(ws + align256((int64_t)256 * sorters * 4));
     const int32_t *keys = buf[0], *tokens = buf[1];
-    if (a.n > kSortShort) {
-        const int64_t tiles = ((int64_t)a.n + kSortThreads - 1) / kSortThreads;
-        const int64_t span = (tiles + blocks - 1) / blocks * kSortThreads;
-        int side = 0;
-        for (int shift = 0; shift == 0 || (a.rows >> shift) > 0; shift += 8) {
-            int32_t *ko = buf[side], *to = buf[side + 1];
-            hipLaunchKernelGGL(k_sort_count, dim3(blocks), dim3(kSortThreads), 0, s, a, keys, shift, shift == 0, span,
-                               hist);
-            hipLaunchKernelGGL(k_sort_place, dim3(blocks), dim3(kSortThreads), 0, s, a, keys, tokens, shift,
-                               shift == 0, span, hist, ko, to);
-            keys = ko;
-            tokens = to;
-            side ^= 2;
-        }
-    } else if (a.n > 0) {
-        hipLaunchKernelGGL(k_sort_short, dim3((a.n + 63) / 64), dim3(kSortThreads), 0, s, a, buf[0], buf[1]);
+    const int64_t tiles = ((int64_t)a.n + kSortThreads - 1) / kSortThreads;
+    const int64_t span = (tiles + sorters - 1) / sorters * kSortThreads;
+    int side = 0;
+    for (int shift = 0; shift == 0 || (a.rows >> shift) > 0; shift += 8) {
+        int32_t *ko = buf[side], *to = buf[side + 1];
+        hipLaunchKernelGGL(k_sort_count, dim3(sorters), dim3(kSortThreads), 0, s, a, keys, shift, shift == 0, span, hist);
+        hipLaunchKernelGGL(k_sort_place, dim3(sorters), dim3(kSortThreads), 0, s, a, keys, tokens, shift, shift == 0,
+                           span, hist, ko, to);
+        keys = ko;
+        tokens = to;
+        side ^= 2;
     }
-    if (a.dtype == KGQ_F32 && a.out_dtype == KGQ_F32) launch_grad<float, float>(a, keys, tokens, piece, s);
-    else if (a.dtype == KGQ_F32) launch_grad<float, uint16_t>(a, keys, tokens, piece, s);
-    else if (a.out_dtype == KGQ_F32) launch_grad<uint16_t, float>(a, keys, tokens, piece, s);
-    else launch_grad<uint16_t, uint16_t>(a, keys, tokens, piece, s);
+    launch_grad<T, O>(a, keys, tokens, piece, s);
+}
+
+}  // namespace
+
+void launch_embed_grad(const EmbedGradArgs& a, hipStream_t s)
+{
+    if (a.dtype == KGQ_F32 && a.out_dtype == KGQ_F32) launch_all<float, float>(a, s);
+    else if (a.dtype == KGQ_F32) launch_all<float, uint16_t>(a, s);
+    else if (a.out_dtype == KGQ_F32) launch_all<uint16_t, float>(a, s);
+    else launch_all<uint16_t, uint16_t>(a, s);
 }
 
 }  // namespace kgq

@@ -1743,6 +1743,7 @@ kgq_status check_workspace(kgq_handle* h, const void* ws, size_t ws_bytes, int64
 
 bool is_dtype(int32_t t) { return t == KGQ_F32 || t == KGQ_BF16; }
 constexpr int32_t kMaxRowBatch = 1 << 20;
+constexpr int32_t kMaxRowDim = 1 << 24;
 
 }  // namespace
 
@@ -1821,7 +1822,7 @@ kgq_status kgq_embed(kgq_handle* h, const void* table, int32_t dtype, int64_t ro
     if (!table || (n && (!ids || !out))) return fail(h, KGQ_E_INVALID_ARG, "table, ids and out must not be NULL");
     if (!is_dtype(dtype) || !is_dtype(out_dtype)) return fail(h, KGQ_E_INVALID_ARG, "unknown dtype");
     if (rows < 1 || rows > 0x7fffffffLL) return fail(h, KGQ_E_INVALID_ARG, "rows outside [1, 2^31-1]");
-    if (dim < 1) return fail(h, KGQ_E_INVALID_ARG, "dim must be >= 1");
+    if (dim < 1 || dim > kMaxRowDim) return fail(h, KGQ_E_INVALID_ARG, "dim outside [1, 2^24]");
     if (ld < dim || ld_out < dim) return fail(h, KGQ_E_INVALID_ARG, "ld and ld_out must be >= dim");
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     DeviceGuard dev;
@@ -1836,7 +1837,8 @@ kgq_status kgq_embed(kgq_handle* h, const void* table, int32_t dtype, int64_t ro
 
 kgq_status kgq_embed_grad_workspace(const kgq_handle* h, int64_t rows, int32_t dim, int32_t n, size_t* bytes)
 {
-    if (!h || !bytes || rows < 1 || rows > 0x7fffffffLL || dim < 1 || n < 0) return KGQ_E_INVALID_ARG;
+    if (!h || !bytes || rows < 1 || rows > 0x7fffffffLL || dim < 1 || dim > kMaxRowDim || n < 0)
+        return KGQ_E_INVALID_ARG;
     *bytes = (size_t)embed_grad_workspace(n, dim);
     return KGQ_OK;
 }
@@ -1850,7 +1852,7 @@ kgq_status kgq_embed_grad(kgq_handle* h, const void* grad, int32_t dtype, int32_
     if (!out || (n && (!ids || !grad))) return fail(h, KGQ_E_INVALID_ARG, "grad, ids and out must not be NULL");
     if (!is_dtype(dtype) || !is_dtype(out_dtype)) return fail(h, KGQ_E_INVALID_ARG, "unknown dtype");
     if (rows < 1 || rows > 0x7fffffffLL) return fail(h, KGQ_E_INVALID_ARG, "rows outside [1, 2^31-1]");
-    if (dim < 1) return fail(h, KGQ_E_INVALID_ARG, "dim must be >= 1");
+    if (dim < 1 || dim > kMaxRowDim) return fail(h, KGQ_E_INVALID_ARG, "dim outside [1, 2^24]");
     if (ld < dim || ld_out < dim) return fail(h, KGQ_E_INVALID_ARG, "ld and ld_out must be >= dim");
     kgq_status st = check_workspace(h, ws, ws_bytes, embed_grad_workspace(n, dim));
     if (st != KGQ_OK) return st;

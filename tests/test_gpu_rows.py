@@ -323,3 +323,26 @@ def test_gpu_embed_grad_one_id_and_padding_alone(eng):
         kept = eng.embed_grad(g, pad, V, out=old.clone(), accumulate=True)
         assert torch.equal(kept, old)
         assert not eng.embed_grad(g, pad, V).any()
+
+
+@pytest.mark.parametrize("n", [2, 64, 65, 2047, 2048, 2049])
+def test_gpu_embed_grad_hot_ids_and_wide_rows(eng, n):
+    """Ids with one token, a handful, and most of them, rows of one column
+    block, two and several; what lies between the output's rows stays."""
+    import torch
+    V = 130
+    rng = np.random.default_rng(n)
+    for d in (1, 256, 257, 512, 513, 1100):
+        ids = np.where(rng.random(n) < 0.5, 129, rng.integers(-1, V, n)).astype(np.int32)
+        g = rng.normal(0, 1, (n, d)).astype(np.float32)
+        for src in ("f32", "bf16"):
+            tg = dev(g, src)
+            big = torch.full((V, d + 3), 7.0, device="cuda")
+            got = host(eng.embed_grad(tg, dev(ids, None), V, scale=0.5, out=big[:, :d]))
+            want, mag = np.zeros((V + 1, d)), np.zeros((V + 1, d))
+            np.add.at(want, ids, host(tg))
+            np.add.at(mag, ids, np.abs(host(tg)))
+            # n additions and the scale, each off by at most 2^-24 of the sum of the magnitudes
+            bound = 0.5 * (n + 1) * 2.0 ** -24 * mag[:V]
+            assert (np.abs(got - 0.5 * want[:V]) <= bound).all(), (n, d, src)
+            assert (big[:, d:] == 7.0).all()

@@ -134,3 +134,14 @@ def test_distill_gradient_is_the_differences():
     h = 1e-6
     up, down = (R.distill(z + s * h * v, idx, t, tau, w)[0] for s in (1, -1))
     np.testing.assert_allclose((w * (up - down)).sum() / (2 * h), (g * v).sum(), rtol=1e-7)
+
+
+def test_row_widths_have_a_limit(eng):
+    """2^24 columns pass every check (and end at the missing device), one more
+    does not."""
+    need = ctypes.c_size_t()
+    n = 1 << 24
+    for d, want in ((n, -5), (n + 1, -1)):
+        assert embed(eng, dim=d, ld=d, ldo=d) == want
+        assert kgq.lib().kgq_embed_grad_workspace(eng.h, 10, d, 4, ctypes.byref(need)) == (0 if want == -5 else -1)
+        assert embed_grad(eng, dim=d, ld=d, ldo=d, ws_bytes=need.value) == want
