@@ -593,9 +593,8 @@ kgq_status kgq_embed(kgq_handle* h, const void* table, int32_t dtype, int64_t ro
  *   ws          device memory, 16-byte aligned, of at least the bytes that
  *               kgq_embed_grad_workspace reports; a call owns it until it has
  *               run, so calls that may overlap need one each
- * Tokens are sorted by id, and the sums are float32 in one order, whatever the
- * timing: results are the same in every call. Rounded once for a bfloat16
- * output.
+ * The rows of an id are added in float32 in one order, whatever the timing:
+ * results are the same in every call. Rounded once for a bfloat16 output.
  * Errors: as kgq_embed, and INVALID_ARG for a ws that is NULL, not aligned or
  * too small. */
 kgq_status kgq_embed_grad_workspace(const kgq_handle* h, int64_t rows, int32_t dim, int32_t n, size_t* bytes);

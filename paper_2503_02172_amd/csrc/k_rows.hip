@@ -146,9 +146,10 @@ void launch_embed_rows(const EmbedArgs& a, hipStream_t s)
 // in token order. Up to kFewAlone of them, a wavefront adds all of a block; more,
 // each adds a share of them, and the shares are added in order. The workgroups
 // behind the tokens' write zeros to the rows whose number they do not find among
-// the ids. 1,536 tokens of 400 to 14,505 rows: 10.6 us (10 without the zeros' 23
-// MB), the latency of a launch, the ids, the rows and one exchange. As many
-// wavefronts as keep the hottest ids short: with four 15.3 us, with 16 16.8.
+// the ids. 1,536 tokens of 400 to 14,505 rows: 10.6 us, in a chain of calls 12
+// (10 without the zeros' 23 MB): the latency of a launch, the ids, the rows and
+// one exchange. As many wavefronts as keep the hottest ids short: with four 15
+// us, with 16, of which most only look for the ids, 17.
 template <typename T, typename O>
 __global__ __launch_bounds__(64 * kFewWaves) void k_grad_few(EmbedGradArgs a, int blocks, int split)
 {
@@ -277,7 +278,7 @@ __device__ __forceinline__ uint32_t token_key(const EmbedGradArgs& a, int64_t i)
 // Least significant digit first, 8 bits a pass, two launches a
 // pass. Block b takes the positions [b * span, (b + 1) * span) tile by tile
 // (one position per thread); hist[b * 256 + digit] is the number of its keys
-// with that digit. The first pass reads the ids themselves. 262,144 tokens: 4.7
+// with that digit. The first pass reads the ids themselves. 262,144 tokens: 4.8
 // us to count and 10.7 to place a pass, bound by latency (a block has two tiles:
 // more blocks would each have more histograms to read).
 __global__ __launch_bounds__(kSortThreads) void k_sort_count(EmbedGradArgs a, const int32_t* keys, int shift, int first,
@@ -412,9 +413,9 @@ __device__ __forceinline__ int lower_bound(const int32_t* keys, int n, uint32_t 
 // The first `sum_blocks` workgroups sum chunks; the others write zeros to the
 // rows without a token. piece: two rows of sums per chunk, of the run that
 // came from the chunk before and of the run that leaves into the next.
-// 262,144 tokens of 400 to 63,361 rows: 112 us, 4.8 TB/s of 419 MB read, 101
+// 262,144 tokens of 400 to 63,361 rows: 111 us, 4.8 TB/s of 419 MB read, 101
 // written and 13 of pieces, the rate of a copy: each token's row is read once,
-// wherever it lies. 1,536 tokens to 14,505 rows: 9 us, the zeros' 23 MB.
+// wherever it lies.
 template <typename T, typename O, bool WIDE>
 __global__ __launch_bounds__(256) void k_grad_chunks(EmbedGradArgs a, GradCut cut, int sum_blocks, const int32_t* keys,
                                                      const int32_t* tokens, float* piece)
@@ -527,7 +528,7 @@ __device__ __forceinline__ void add_pieces(const float* rest, int d, int lo, int
 // pieces by itself; the workgroup then takes the longer runs of its 16 chunks
 // together (each wavefront a share of the pieces, the shares added in order).
 // 262,144 tokens, log-uniform ids: 13 us (the whole gradient 160; 203 if the
-// workgroup takes every run); 1,536: 6 us, a chain of four loads.
+// workgroup takes every run); of few chunks 6 us, a chain of four loads.
 template <typename O>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_grad_join(EmbedGradArgs a, GradCut cut, const int32_t* keys,
                                                                const float* piece)
@@ -612,8 +613,8 @@ int sort_blocks(int64_t n)
 }
 
 // Groups of just enough lanes for a row, 16 bytes a lane, and chunks that give
-// the chip some 16 wavefronts a compute unit: 8 to 64 tokens (1,536 tokens of
-// 400: 22 us with 8, 40 with 64; 262,144: 160 us with 64, 228 with 8; longer ones
+// the chip some 16 wavefronts a compute unit: 8 to 64 tokens (5,000 tokens of
+// 400: 31 us with 8, 49 with 64; 262,144: 160 us with 64, 228 with 8; longer ones
 // would save pieces, one or two rows a chunk, that are few beside 64 already).
 // The element size is the smaller of the two types', so that the workspace
 // holds either.
