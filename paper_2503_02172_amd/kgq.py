@@ -357,30 +357,38 @@ class Engine:
 
     # -- drawing, distillation, embedding rows ----------------------------------
     def _rows_stream(self, stream, inputs):
-        """(raw stream, allocator on it) of a call; with a stream of the
-        caller's, inputs' memory outlives the work on it."""
+        """(raw stream, on) of a call: on(f, ...) is f(...) with torch's work and
+        memory on that stream. With a stream of the caller's, inputs' memory
+        outlives the work on it."""
         import torch
         if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream, torch.empty
+            return torch.cuda.current_stream(self.device).cuda_stream, lambda f, *args, **kw: f(*args, **kw)
         dev = torch.device("cuda", self.device)
         ts = torch.cuda.ExternalStream(stream, device=dev) if isinstance(stream, int) else stream
         for t in inputs:
             if t is not None:
                 t.record_stream(ts)
 
-        def empty(*shape, **kw):
+        def on(f, *args, **kw):
             with torch.cuda.stream(ts):
-                return torch.empty(*shape, **kw)
-        return ts.cuda_stream, empty
+                return f(*args, **kw)
+        return ts.cuda_stream, on
+
+    def _element(self, call: str, name: str, t):
+        """dtype of a float32 or bfloat16 tensor on the handle's device."""
+        import torch
+        dt = F32 if t.dtype == torch.float32 else BF16 if t.dtype == torch.bfloat16 else None
+        if dt is None or not t.is_cuda:
+            raise TypeError(f"{call}: {name} must be a float32 or bfloat16 CUDA tensor")
+        if t.device.index != self.device:
+            raise ValueError(f"{call}: {name} is not on the handle's device")
+        return dt
 
     def _matrix(self, call: str, name: str, t, width: Optional[int] = None):
         """(dtype, row stride) of a float32 or bfloat16 matrix on the handle's device."""
-        import torch
-        dt = F32 if t.dtype == torch.float32 else BF16 if t.dtype == torch.bfloat16 else None
-        if dt is None or t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
-            raise TypeError(f"{call}: {name} must be a float32 or bfloat16 CUDA matrix with unit column stride")
-        if t.device.index != self.device:
-            raise ValueError(f"{call}: {name} is not on the handle's device")
+        dt = self._element(call, name, t)
+        if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise TypeError(f"{call}: {name} must be a matrix with unit column stride")
         if width is not None and t.shape[1] != width:
             raise ValueError(f"{call}: {name} must have {width} columns")
         # (the stride of a single row is never used)
@@ -421,10 +429,10 @@ class Engine:
         rc = lib().kgq_sample_workspace(self.h, B, ctypes.byref(need))
         if rc != OK:
             raise KgqError(rc, "sample: batch outside [1, 2^20]")
-        raw, empty = self._rows_stream(stream, kept)
-        idx = empty(u.shape, dtype=torch.int32, device=u.device)
-        lp = empty(u.shape, dtype=torch.float32, device=u.device) if logp else None
-        ws = empty(need.value, dtype=torch.uint8, device=u.device)
+        raw, on = self._rows_stream(stream, kept)
+        idx = on(torch.empty, u.shape, dtype=torch.int32, device=u.device)
+        lp = on(torch.empty, u.shape, dtype=torch.float32, device=u.device) if logp else None
+        ws = on(torch.empty, need.value, dtype=torch.uint8, device=u.device)
         self._check(lib().kgq_sample(self.h, B, _ptr(scores), dt, ld, ctypes.byref(how), _ptr(u), u.shape[1],
                                      _ptr(idx), _ptr(lp), _ptr(ws), need.value, raw))
         return idx, lp
@@ -455,10 +463,10 @@ class Engine:
                    ((scores, ld), (out, ld_grad))]
             if not same and out.data_ptr() < end[0] and scores.data_ptr() < end[1]:
                 raise ValueError("distill: out overlaps scores and is not the same matrix")
-        raw, empty = self._rows_stream(stream, (scores, idx, score, weight, out))
-        ls = empty(B, dtype=torch.float32, device=scores.device) if loss else None
+        raw, on = self._rows_stream(stream, (scores, idx, score, weight, out))
+        ls = on(torch.empty, B, dtype=torch.float32, device=scores.device) if loss else None
         if grad and out is None:
-            out = empty((B, self.n_entities), dtype=scores.dtype, device=scores.device)
+            out = on(torch.empty, (B, self.n_entities), dtype=scores.dtype, device=scores.device)
             ld_grad = self.n_entities
         g = out if grad else None
         self._check(lib().kgq_distill(self.h, B, _ptr(scores), dt, ld, idx.shape[1], _ptr(idx), _ptr(score),
@@ -476,8 +484,8 @@ class Engine:
         dtype = dtype or table.dtype
         if dtype not in (torch.float32, torch.bfloat16):
             raise TypeError("embed: dtype must be float32 or bfloat16")
-        raw, empty = self._rows_stream(stream, (table, ids))
-        out = empty(tuple(ids.shape) + (d,), dtype=dtype, device=table.device)
+        raw, on = self._rows_stream(stream, (table, ids))
+        out = on(torch.empty, tuple(ids.shape) + (d,), dtype=dtype, device=table.device)
         self._check(lib().kgq_embed(self.h, _ptr(table), dt, table.shape[0], d, ld, _ptr(ids), ids.numel(), scale,
                                     _ptr(out), F32 if dtype == torch.float32 else BF16, d, raw))
         return out
@@ -492,10 +500,8 @@ class Engine:
         self._array("embed_grad", "ids", ids, torch.int32, None)
         if tuple(grad.shape[:-1]) != tuple(ids.shape):
             raise ValueError("embed_grad: grad must have shape ids.shape + (d,)")
-        if grad.dim() != 2:
-            grad = grad.reshape(-1, grad.shape[-1])
-        dt, ld = self._matrix("embed_grad", "grad", grad)
-        n, d = grad.shape
+        self._element("embed_grad", "grad", grad)
+        n, d = ids.numel(), grad.shape[-1]
         if accumulate and out is None:
             raise ValueError("embed_grad: accumulate needs out")
         if out is not None:
@@ -507,13 +513,18 @@ class Engine:
             if dtype not in (torch.float32, torch.bfloat16):
                 raise TypeError("embed_grad: dtype must be float32 or bfloat16")
             odt, ld_out = (F32 if dtype == torch.float32 else BF16), d
+        raw, on = self._rows_stream(stream, (grad, ids, out))
+        if grad.dim() != 2:
+            # (a copy where the rows have no common stride: on the call's stream,
+            # so that the kernels run behind it)
+            grad = on(grad.reshape, n, d)
+        dt, ld = self._matrix("embed_grad", "grad", grad)
         need = ctypes.c_size_t()
         if lib().kgq_embed_grad_workspace(self.h, rows, d, n, ctypes.byref(need)) != OK:
             raise ValueError("embed_grad: rows, d or the number of ids is out of range")
-        raw, empty = self._rows_stream(stream, (grad, ids, out))
         if out is None:
-            out = empty((rows, d), dtype=dtype, device=grad.device)
-        ws = empty(need.value, dtype=torch.uint8, device=grad.device)
+            out = on(torch.empty, (rows, d), dtype=dtype, device=grad.device)
+        ws = on(torch.empty, need.value, dtype=torch.uint8, device=grad.device)
         self._check(lib().kgq_embed_grad(self.h, _ptr(grad), dt, n, d, ld, _ptr(ids), rows, scale, _ptr(out), odt,
                                          ld_out, int(accumulate), _ptr(ws), need.value, raw))
         return out

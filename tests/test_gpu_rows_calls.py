@@ -1,0 +1,45 @@
+"""Calls that the documentation of drawing, distillation and embedding rows
+allows beyond the plain ones: gradients in layouts that have to be copied, on
+streams of the caller's."""
+
+import numpy as np
+import pytest
+
+from paper_2503_02172_amd import kgq
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def eng():
+    e = kgq.Engine(kgq.GQE, 16, 1, 4, 24.0, 1)
+    yield e
+    e.close()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n", [40, 400])
+def test_gpu_embed_grad_copies_on_the_callers_stream(eng, n, dtype):
+    """Gradients whose rows have no common stride, on a stream of the
+    caller's, while the current stream is busy: the sums are those of the
+    gradient, whatever the current stream is at. Whole numbers, so that sums
+    are exact in any order."""
+    import torch
+    rng = np.random.default_rng(n)
+    T, V, d = 9, 50, 24
+    ids = torch.as_tensor(rng.integers(-1, V, (T, n)).astype(np.int32), device="cuda")
+    whole = torch.as_tensor(rng.integers(-8, 9, (T, n + 1, d)), device="cuda").to(getattr(torch, dtype))
+    turned = whole.transpose(0, 1).contiguous().transpose(0, 1)
+    a = torch.randn(4096, 4096, device="cuda")
+    s = torch.cuda.Stream()
+    for layout, g in (("rows cut off", whole[:, 1:]), ("transposed", turned[:, :-1]), ("flat", whole[:, 1:].contiguous())):
+        want = np.zeros((V + 1, d))
+        np.add.at(want, ids.cpu().numpy().ravel(), g.double().cpu().numpy().reshape(-1, d))
+        for stream in (s, s.cuda_stream, None):
+            torch.cuda.synchronize()
+            s.wait_stream(torch.cuda.current_stream())
+            for _ in range(20):
+                a = (a @ a).clamp_(-1, 1)                      # (what the copy must not wait for)
+            got = eng.embed_grad(g, ids, V, stream=stream)
+            torch.cuda.synchronize()
+            assert np.array_equal(got.double().cpu().numpy(), want[:V]), (layout, stream)

@@ -1,0 +1,67 @@
+"""What the binding does around the calls on the caller's own arrays (draws,
+distillation, embedding rows), on a validation-only handle: the checks of type
+and device are switched off, so that host tensors take the way of device ones
+up to the library, which ends at the missing device."""
+
+import contextlib
+
+import pytest
+import torch
+
+from paper_2503_02172_amd import kgq
+
+COPIES = ("clone", "copy_", "_to_copy")
+
+
+@pytest.fixture
+def eng(monkeypatch):
+    monkeypatch.setattr(kgq.Engine, "_element", lambda self, call, name, t: kgq.F32, raising=False)
+    monkeypatch.setattr(kgq.Engine, "_matrix", lambda self, call, name, t, width=None: (kgq.F32, t.stride(0)))
+    monkeypatch.setattr(kgq.Engine, "_array", lambda *a: None)
+    e = kgq.Engine(kgq.GQE, 50, 6, 8, 12.0, 4, device=-1)
+    e.device = 0                                               # (what streams are asked for; the handle has none)
+    return e
+
+
+class CallersStream:
+    cuda_stream = 4096
+
+
+class Copies(torch.utils._python_dispatch.TorchDispatchMode):
+    """The copies that are made, each with the stream that it is made on."""
+
+    def __init__(self, on):
+        super().__init__()
+        self.on, self.made = on, []
+
+    def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+        if func.overloadpacket.__name__ in COPIES:
+            self.made.append(self.on[-1])
+        return func(*args, **(kwargs or {}))
+
+
+@pytest.mark.parametrize("layout", ["rows cut off", "transposed", "flat"])
+def test_a_gradients_copy_is_made_on_the_calls_stream(eng, monkeypatch, layout):
+    """A gradient whose rows have no common stride is copied; the kernels run
+    behind that copy only if both are on one stream."""
+    on = [None]
+
+    @contextlib.contextmanager
+    def stream(s):
+        on.append(s)
+        yield
+        on.pop()
+
+    kept = []
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: kept.append((t, s)))
+    grad = {"rows cut off": torch.zeros(4, 6, 8)[:, 1:], "transposed": torch.zeros(5, 4, 8).transpose(0, 1),
+            "flat": torch.zeros(4, 5, 8)}[layout]
+    ids = torch.zeros(4, 5, dtype=torch.int32)
+    mine = CallersStream()
+    with Copies(on) as copies, pytest.raises(kgq.KgqError) as e:
+        eng.embed_grad(grad, ids, 10, stream=mine)
+    assert e.value.name == "NO_DEVICE"                         # everything else passed
+    assert copies.made == ([] if layout == "flat" else [mine])
+    # the caller's own memory outlives the work on it
+    assert any(t.data_ptr() == grad.data_ptr() and s is mine for t, s in kept)
