@@ -147,6 +147,13 @@ def _ptr(t) -> int:
     return int(t.ctypes.data)
 
 
+def _int32(call: str, **values):
+    """Refuses numbers that ctypes would cut to the library's 32-bit integers."""
+    for name, v in values.items():
+        if not -1 << 31 <= v < 1 << 31:
+            raise ValueError(f"{call}: {name} = {v} does not fit 32 bits")
+
+
 def _stream(stream) -> int:
     if stream is None:
         import torch
@@ -423,6 +430,7 @@ class Engine:
                 rows[name] = value.data_ptr()
                 settings[name] = 1                                 # (in every range; not used)
                 kept.append(value)
+        _int32("sample", batch=B, draws=u.shape[1], top_k=settings["top_k"])
         how = Sampling(settings["temperature"], settings["top_p"], settings["min_p"], settings["top_k"],
                        rows.get("temperature"), rows.get("top_k"), rows.get("top_p"), rows.get("min_p"))
         need = ctypes.c_size_t()
@@ -449,6 +457,7 @@ class Engine:
         B = scores.shape[0]
         if idx.dim() != 2:
             raise ValueError("distill: idx must be [B x k]")
+        _int32("distill", batch=B, k=idx.shape[1])
         self._array("distill", "idx", idx, torch.int32, (B, idx.shape[1]))
         self._array("distill", "score", score, torch.float32, (B, idx.shape[1]))
         if weight is not None:
@@ -480,13 +489,14 @@ class Engine:
         import torch
         dt, ld = self._matrix("embed", "table", table)
         self._array("embed", "ids", ids, torch.int32, None)
-        d = table.shape[1]
+        n, d = ids.numel(), table.shape[1]
+        _int32("embed", ids=n, columns=d)
         dtype = dtype or table.dtype
         if dtype not in (torch.float32, torch.bfloat16):
             raise TypeError("embed: dtype must be float32 or bfloat16")
         raw, on = self._rows_stream(stream, (table, ids))
         out = on(torch.empty, tuple(ids.shape) + (d,), dtype=dtype, device=table.device)
-        self._check(lib().kgq_embed(self.h, _ptr(table), dt, table.shape[0], d, ld, _ptr(ids), ids.numel(), scale,
+        self._check(lib().kgq_embed(self.h, _ptr(table), dt, table.shape[0], d, ld, _ptr(ids), n, scale,
                                     _ptr(out), F32 if dtype == torch.float32 else BF16, d, raw))
         return out
 
@@ -502,6 +512,7 @@ class Engine:
             raise ValueError("embed_grad: grad must have shape ids.shape + (d,)")
         self._element("embed_grad", "grad", grad)
         n, d = ids.numel(), grad.shape[-1]
+        _int32("embed_grad", ids=n, columns=d)
         if accumulate and out is None:
             raise ValueError("embed_grad: accumulate needs out")
         if out is not None:

@@ -40,6 +40,32 @@ class Copies(torch.utils._python_dispatch.TorchDispatchMode):
         return func(*args, **(kwargs or {}))
 
 
+BEYOND = (1 << 32) + 5                                         # 5, if cut to 32 bits
+
+
+@pytest.mark.parametrize("what", ["embed ids", "embed columns", "embed_grad ids", "embed_grad columns", "sample rows",
+                                  "sample draws", "sample top_k", "distill rows", "distill k"])
+def test_sizes_beyond_32_bits_are_refused(eng, monkeypatch, what):
+    """Counts that the library takes as 32-bit integers are not cut to them."""
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: pytest.fail("memory asked for"))
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: None)
+    f = lambda *shape: torch.zeros(1).expand(*shape)
+    i = lambda *shape: torch.zeros(1, dtype=torch.int32).expand(*shape)
+    call = {
+        "embed ids": lambda s: eng.embed(f(4, 8), i(BEYOND), stream=s),
+        "embed columns": lambda s: eng.embed(f(1, BEYOND), i(3), stream=s),
+        "embed_grad ids": lambda s: eng.embed_grad(f(BEYOND, 8), i(BEYOND), 10, stream=s),
+        "embed_grad columns": lambda s: eng.embed_grad(f(3, BEYOND), i(3), 10, stream=s),
+        "sample rows": lambda s: eng.sample(f(BEYOND, 50), f(BEYOND, 3), stream=s),
+        "sample draws": lambda s: eng.sample(f(2, 50), f(2, BEYOND), stream=s),
+        "sample top_k": lambda s: eng.sample(f(2, 50), f(2, 3), top_k=BEYOND, stream=s),
+        "distill rows": lambda s: eng.distill(f(BEYOND, 50), i(BEYOND, 3), f(BEYOND, 3), stream=s),
+        "distill k": lambda s: eng.distill(f(2, 50), i(2, BEYOND), f(2, BEYOND), stream=s),
+    }[what]
+    with pytest.raises(ValueError, match="32 bits"):
+        call(CallersStream())
+
+
 @pytest.mark.parametrize("layout", ["rows cut off", "transposed", "flat"])
 def test_a_gradients_copy_is_made_on_the_calls_stream(eng, monkeypatch, layout):
     """A gradient whose rows have no common stride is copied; the kernels run
