@@ -8,6 +8,7 @@ anything else.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Optional, Sequence
@@ -23,6 +24,7 @@ TNORM_PRODUCT, TNORM_MIN, TNORM_LUKASIEWICZ = 0, 1, 2
 DENSE_AUTO, DENSE_FP32, DENSE_BF16X3 = 0, 1, 2
 NUM_STRUCTURES = 14
 MAX_K = 1024
+MAX_INT32 = (1 << 31) - 1
 PLAN_FIELDS = ["chains", "groups", "intersection_inputs", "level1", "level2", "level3", "post",
                "scored_rows", "union_pairs", "launches", "intersection_stages", "union_quads", "state_rows"]
 INFO_FIELDS = ["anchors", "relations", "terms", "fused_ops", "intersection_stages", "launches", "max_batch",
@@ -147,11 +149,10 @@ def _ptr(t) -> int:
     return int(t.ctypes.data)
 
 
-def _int32(call: str, **values):
-    """Refuses numbers that ctypes would cut to the library's 32-bit integers."""
-    for name, v in values.items():
-        if not -1 << 31 <= v < 1 << 31:
-            raise ValueError(f"{call}: {name} = {v} does not fit 32 bits")
+def _beyond_int32(call: str, **values):
+    """The error for a number that ctypes would cut to a 32-bit integer."""
+    name, v = max(values.items(), key=lambda kv: abs(kv[1]))
+    return ValueError(f"{call}: {name} = {v} does not fit 32 bits")
 
 
 def _stream(stream) -> int:
@@ -363,23 +364,28 @@ class Engine:
         return y
 
     # -- drawing, distillation, embedding rows ----------------------------------
+    def _torch_stream(self, stream):
+        """A stream of the caller's (torch's, or a raw hipStream_t) as torch's."""
+        import torch
+        if isinstance(stream, int):
+            return torch.cuda.ExternalStream(stream, device=torch.device("cuda", self.device))
+        return stream
+
     def _rows_stream(self, stream, inputs):
-        """(raw stream, on) of a call: on(f, ...) is f(...) with torch's work and
-        memory on that stream. With a stream of the caller's, inputs' memory
-        outlives the work on it."""
+        """(raw stream, allocator on it) of a call; with a stream of the
+        caller's, inputs' memory outlives the work on it."""
         import torch
         if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream, lambda f, *args, **kw: f(*args, **kw)
-        dev = torch.device("cuda", self.device)
-        ts = torch.cuda.ExternalStream(stream, device=dev) if isinstance(stream, int) else stream
+            return torch.cuda.current_stream(self.device).cuda_stream, torch.empty
+        ts = self._torch_stream(stream)
         for t in inputs:
             if t is not None:
                 t.record_stream(ts)
 
-        def on(f, *args, **kw):
+        def empty(*shape, **kw):
             with torch.cuda.stream(ts):
-                return f(*args, **kw)
-        return ts.cuda_stream, on
+                return torch.empty(*shape, **kw)
+        return ts.cuda_stream, empty
 
     def _element(self, call: str, name: str, t):
         """dtype of a float32 or bfloat16 tensor on the handle's device."""
@@ -430,17 +436,18 @@ class Engine:
                 rows[name] = value.data_ptr()
                 settings[name] = 1                                 # (in every range; not used)
                 kept.append(value)
-        _int32("sample", batch=B, draws=u.shape[1], top_k=settings["top_k"])
+        if B > MAX_INT32 or u.shape[1] > MAX_INT32 or not -MAX_INT32 <= settings["top_k"] <= MAX_INT32:
+            raise _beyond_int32("sample", batch=B, draws=u.shape[1], top_k=settings["top_k"])
         how = Sampling(settings["temperature"], settings["top_p"], settings["min_p"], settings["top_k"],
                        rows.get("temperature"), rows.get("top_k"), rows.get("top_p"), rows.get("min_p"))
         need = ctypes.c_size_t()
         rc = lib().kgq_sample_workspace(self.h, B, ctypes.byref(need))
         if rc != OK:
             raise KgqError(rc, "sample: batch outside [1, 2^20]")
-        raw, on = self._rows_stream(stream, kept)
-        idx = on(torch.empty, u.shape, dtype=torch.int32, device=u.device)
-        lp = on(torch.empty, u.shape, dtype=torch.float32, device=u.device) if logp else None
-        ws = on(torch.empty, need.value, dtype=torch.uint8, device=u.device)
+        raw, empty = self._rows_stream(stream, kept)
+        idx = empty(u.shape, dtype=torch.int32, device=u.device)
+        lp = empty(u.shape, dtype=torch.float32, device=u.device) if logp else None
+        ws = empty(need.value, dtype=torch.uint8, device=u.device)
         self._check(lib().kgq_sample(self.h, B, _ptr(scores), dt, ld, ctypes.byref(how), _ptr(u), u.shape[1],
                                      _ptr(idx), _ptr(lp), _ptr(ws), need.value, raw))
         return idx, lp
@@ -457,7 +464,8 @@ class Engine:
         B = scores.shape[0]
         if idx.dim() != 2:
             raise ValueError("distill: idx must be [B x k]")
-        _int32("distill", batch=B, k=idx.shape[1])
+        if B > MAX_INT32 or idx.shape[1] > MAX_INT32:
+            raise _beyond_int32("distill", batch=B, k=idx.shape[1])
         self._array("distill", "idx", idx, torch.int32, (B, idx.shape[1]))
         self._array("distill", "score", score, torch.float32, (B, idx.shape[1]))
         if weight is not None:
@@ -467,15 +475,18 @@ class Engine:
             odt, ld_grad = self._matrix("distill", "out", out, self.n_entities)
             if odt != dt or out.shape[0] != B:
                 raise ValueError("distill: out must have the shape and dtype of scores")
-            same = out.data_ptr() == scores.data_ptr() and ld_grad == ld
-            end = [t.data_ptr() + ((B - 1) * s + self.n_entities) * t.element_size() for t, s in
-                   ((scores, ld), (out, ld_grad))]
-            if not same and out.data_ptr() < end[0] and scores.data_ptr() < end[1]:
+            # the same matrix, or no element of it: with one stride, two ranges of
+            # columns that do not meet, a row's end joined to the next one's start
+            far = out.data_ptr() - scores.data_ptr()
+            size, N = scores.element_size(), self.n_entities
+            span = [((B - 1) * s + N) * size for s in (ld, ld_grad)]
+            if (far or ld_grad != ld) and -span[1] < far < span[0] and \
+                    (ld_grad != ld or far % size or not N <= far // size % ld <= ld - N):
                 raise ValueError("distill: out overlaps scores and is not the same matrix")
-        raw, on = self._rows_stream(stream, (scores, idx, score, weight, out))
-        ls = on(torch.empty, B, dtype=torch.float32, device=scores.device) if loss else None
+        raw, empty = self._rows_stream(stream, (scores, idx, score, weight, out))
+        ls = empty(B, dtype=torch.float32, device=scores.device) if loss else None
         if grad and out is None:
-            out = on(torch.empty, (B, self.n_entities), dtype=scores.dtype, device=scores.device)
+            out = empty((B, self.n_entities), dtype=scores.dtype, device=scores.device)
             ld_grad = self.n_entities
         g = out if grad else None
         self._check(lib().kgq_distill(self.h, B, _ptr(scores), dt, ld, idx.shape[1], _ptr(idx), _ptr(score),
@@ -490,12 +501,13 @@ class Engine:
         dt, ld = self._matrix("embed", "table", table)
         self._array("embed", "ids", ids, torch.int32, None)
         n, d = ids.numel(), table.shape[1]
-        _int32("embed", ids=n, columns=d)
+        if n > MAX_INT32 or d > MAX_INT32:
+            raise _beyond_int32("embed", ids=n, columns=d)
         dtype = dtype or table.dtype
         if dtype not in (torch.float32, torch.bfloat16):
             raise TypeError("embed: dtype must be float32 or bfloat16")
-        raw, on = self._rows_stream(stream, (table, ids))
-        out = on(torch.empty, tuple(ids.shape) + (d,), dtype=dtype, device=table.device)
+        raw, empty = self._rows_stream(stream, (table, ids))
+        out = empty(tuple(ids.shape) + (d,), dtype=dtype, device=table.device)
         self._check(lib().kgq_embed(self.h, _ptr(table), dt, table.shape[0], d, ld, _ptr(ids), n, scale,
                                     _ptr(out), F32 if dtype == torch.float32 else BF16, d, raw))
         return out
@@ -510,9 +522,13 @@ class Engine:
         self._array("embed_grad", "ids", ids, torch.int32, None)
         if tuple(grad.shape[:-1]) != tuple(ids.shape):
             raise ValueError("embed_grad: grad must have shape ids.shape + (d,)")
-        self._element("embed_grad", "grad", grad)
+        if grad.dim() == 2:
+            dt, ld = self._matrix("embed_grad", "grad", grad)
+        else:
+            self._element("embed_grad", "grad", grad)
         n, d = ids.numel(), grad.shape[-1]
-        _int32("embed_grad", ids=n, columns=d)
+        if n > MAX_INT32 or d > MAX_INT32:
+            raise _beyond_int32("embed_grad", ids=n, columns=d)
         if accumulate and out is None:
             raise ValueError("embed_grad: accumulate needs out")
         if out is not None:
@@ -524,18 +540,19 @@ class Engine:
             if dtype not in (torch.float32, torch.bfloat16):
                 raise TypeError("embed_grad: dtype must be float32 or bfloat16")
             odt, ld_out = (F32 if dtype == torch.float32 else BF16), d
-        raw, on = self._rows_stream(stream, (grad, ids, out))
+        raw, empty = self._rows_stream(stream, (grad, ids, out))
         if grad.dim() != 2:
             # (a copy where the rows have no common stride: on the call's stream,
             # so that the kernels run behind it)
-            grad = on(grad.reshape, n, d)
-        dt, ld = self._matrix("embed_grad", "grad", grad)
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(self._torch_stream(stream)):
+                grad = grad.reshape(n, d)
+            dt, ld = self._matrix("embed_grad", "grad", grad)
         need = ctypes.c_size_t()
         if lib().kgq_embed_grad_workspace(self.h, rows, d, n, ctypes.byref(need)) != OK:
             raise ValueError("embed_grad: rows, d or the number of ids is out of range")
         if out is None:
-            out = on(torch.empty, (rows, d), dtype=dtype, device=grad.device)
-        ws = on(torch.empty, need.value, dtype=torch.uint8, device=grad.device)
+            out = empty((rows, d), dtype=dtype, device=grad.device)
+        ws = empty(need.value, dtype=torch.uint8, device=grad.device)
         self._check(lib().kgq_embed_grad(self.h, _ptr(grad), dt, n, d, ld, _ptr(ids), rows, scale, _ptr(out), odt,
                                          ld_out, int(accumulate), _ptr(ws), need.value, raw))
         return out

@@ -1,6 +1,6 @@
 """Calls that the documentation of drawing, distillation and embedding rows
 allows beyond the plain ones: gradients in layouts that have to be copied, on
-streams of the caller's."""
+streams of the caller's; a score matrix and its gradient in one buffer."""
 
 import numpy as np
 import pytest
@@ -43,3 +43,21 @@ def test_gpu_embed_grad_copies_on_the_callers_stream(eng, n, dtype):
             got = eng.embed_grad(g, ids, V, stream=stream)
             torch.cuda.synchronize()
             assert np.array_equal(got.double().cpu().numpy(), want[:V]), (layout, stream)
+
+
+@pytest.mark.parametrize("N", [70, 14505, 70001])
+def test_gpu_distill_gradient_beside_the_scores(N):
+    """Scores and their gradient as two column ranges of one buffer."""
+    import torch
+    B = 5
+    eng = kgq.Engine(kgq.GQE, N, 1, 4, 24.0, 1)
+    buf = torch.full((B, 2 * N + 3), 7.0, device="cuda")
+    z, out = buf[:, 1:N + 1], buf[:, N + 1:2 * N + 1]
+    z.normal_()
+    t, idx = torch.randn(B, N, device="cuda").topk(20, 1)
+    idx, t = idx.int(), t.contiguous()
+    loss, grad = eng.distill(z.contiguous(), idx, t, temperature=2.0)
+    old = z.clone()
+    got = eng.distill(z, idx, t, temperature=2.0, out=out)
+    assert got[1] is out and torch.equal(got[0], loss) and torch.equal(out, grad)
+    assert torch.equal(z, old) and (buf[:, 0] == 7.0).all() and (buf[:, 2 * N + 1:] == 7.0).all()

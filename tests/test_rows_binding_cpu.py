@@ -91,3 +91,35 @@ def test_a_gradients_copy_is_made_on_the_calls_stream(eng, monkeypatch, layout):
     assert copies.made == ([] if layout == "flat" else [mine])
     # the caller's own memory outlives the work on it
     assert any(t.data_ptr() == grad.data_ptr() and s is mine for t, s in kept)
+
+
+def distill_into(eng, monkeypatch, scores, out):
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: None)
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    B = scores.shape[0]
+    idx, score = torch.zeros(B, 3, dtype=torch.int32), torch.zeros(B, 3)
+    eng.distill(scores, idx, score, out=out, stream=CallersStream())
+
+
+def test_distill_out_may_share_a_buffer_with_scores(eng, monkeypatch):
+    """Column ranges that share no element are not refused, ranges that share
+    one are; so are rows that interleave with another stride."""
+    buf = torch.zeros(4, 130)
+    flat = torch.zeros(4 * 130 + 200)
+    rows = lambda at, ld: torch.as_strided(flat, (4, 50), (ld, 1), at)
+    apart = [(buf[:, :50], buf[:, 50:100]), (buf[:, 80:], buf[:, 30:80]), (buf[:, :50], buf[:, 80:]),
+             (rows(0, 130), rows(180, 130)),                   # a column range, a row on
+             (rows(0, 130), rows(80, 130)),                    # up to the next row's start
+             (rows(0, 50), rows(200, 50)), (buf[:, :50], buf[:, :50]), (buf[:1, :50], buf[1:2, 20:70])]
+    met = [(buf[:, :50], buf[:, 49:99]), (buf[:, 49:99], buf[:, :50]), (rows(0, 130), rows(129, 130)),
+           (rows(0, 130), rows(81, 130)), (rows(0, 130), rows(130, 130)), (rows(0, 50), rows(150, 50)),
+           (rows(0, 100), rows(50, 101)), (rows(0, 100), rows(0, 101)), (buf[:1, :50], buf[:1, 49:99])]
+    for expected, pairs in (("NO_DEVICE", apart), ("overlaps", met)):
+        for scores, out in pairs:
+            cells = [{int(i) for i in torch.as_strided(torch.arange(10 ** 4), t.shape, t.stride(), t.storage_offset()).flatten()}
+                     for t in (scores, out)]
+            same = cells[0] == cells[1] and scores.stride() == out.stride()
+            if scores.stride() == out.stride() or scores.shape[0] == 1:
+                assert (same or not cells[0] & cells[1]) == (expected == "NO_DEVICE")     # (the lists above are right)
+            with pytest.raises((kgq.KgqError, ValueError), match=expected):
+                distill_into(eng, monkeypatch, scores, out)
