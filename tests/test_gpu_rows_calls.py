@@ -1,6 +1,7 @@
 """Calls that the documentation of drawing, distillation and embedding rows
 allows beyond the plain ones: gradients in layouts that have to be copied, on
-streams of the caller's; a score matrix and its gradient in one buffer."""
+streams of the caller's; a score matrix and its gradient in one buffer.
+And gradients whose sums are exact, so that a token left out shows."""
 
 import numpy as np
 import pytest
@@ -61,3 +62,36 @@ def test_gpu_distill_gradient_beside_the_scores(N):
     got = eng.distill(z, idx, t, temperature=2.0, out=out)
     assert got[1] is out and torch.equal(got[0], loss) and torch.equal(out, grad)
     assert torch.equal(z, old) and (buf[:, 0] == 7.0).all() and (buf[:, 2 * N + 1:] == 7.0).all()
+
+
+def odd_rows(n, d, seed):
+    """Odd numbers from -7 to 7: every sum of up to 2^21 of them is exact in
+    float32 in any order, and a row left out or added twice changes it."""
+    return 2.0 * np.random.default_rng(seed).integers(-4, 4, (n, d)) + 1.0
+
+
+@pytest.mark.parametrize("src", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,d", [(9, 3), (10, 300), (513, 1100), (2047, 8), (2048, 300), (2049, 8), (4097, 300),
+                                 (9000, 6), (33333, 1100), (100000, 3), (262143, 40)])
+def test_gpu_embed_grad_of_hot_ids_is_exact(eng, n, d, src):
+    """Ids with most of the tokens, alone and between others, in one run or
+    several, written and accumulated: every token counts once."""
+    import torch
+    V = 300
+    g = odd_rows(n, d, n)
+    tg = torch.as_tensor(g, device="cuda").to(getattr(torch, src))
+    rng = np.random.default_rng(n + 1)
+    at = np.arange(n)
+    kinds = {"one": np.full(n, V // 2), "last": np.full(n, V - 1), "two": at % 2 * 7,
+             "three quarters": np.where(at % 4 == 0, rng.integers(-1, V, n), 17), "halves": np.where(at < n // 2, 3, 4),
+             "all but one": np.where(at == n // 3, 200, 100), "runs": at // 2500 % V,
+             "padding between": np.where(at % 5 == 0, -1, 299)}
+    for kind, ids in kinds.items():
+        ti = torch.as_tensor(ids.astype(np.int32), device="cuda")
+        want = np.zeros((V + 1, d))
+        np.add.at(want, ids, g)
+        got = eng.embed_grad(tg, ti, V, scale=0.5)
+        assert np.array_equal(got.double().cpu().numpy(), 0.5 * want[:V]), kind
+        old = torch.as_tensor(rng.integers(-9, 9, (V, d)), device="cuda").float()
+        acc = eng.embed_grad(tg, ti, V, scale=-2.0, out=old.clone(), accumulate=True)
+        assert np.array_equal(acc.double().cpu().numpy(), old.double().cpu().numpy() - 2.0 * want[:V]), kind
