@@ -524,8 +524,12 @@ kgq_status kgq_sample_workspace(const kgq_handle* h, int32_t batch, size_t* byte
  *   ws        device memory, 16-byte aligned, of at least the bytes that
  *             kgq_sample_workspace reports; a call owns it until it has run, so
  *             calls that may overlap need one each
- * Weights and their sums are in double precision; results are the same in
- * every call.
+ * Weights are doubles with a relative error of up to 4e-14, and those below
+ * 2^-1000 of the largest count as 0. Their sums are doubles; where top-p's
+ * border falls among very many equal or nearly equal scores, sums in fixed
+ * point find it, to n_entities 2^-61 of the weight. A cut or a draw differs from
+ * the definition's only where its border lies that close to another entity.
+ * Results are the same in every call.
  * Errors: INVALID_ARG (NULL scores, how, u or out_idx, unknown dtype, batch
  * outside [1, 2^20], n_draws < 1, ld < n_entities, a setting outside its
  * range, ws NULL, not aligned or too small; checked mode under capture), NO_DEVICE, DEVICE. */
