@@ -552,7 +552,9 @@ kgq_status kgq_sample(kgq_handle* h, int32_t batch, const void* scores, int32_t 
  *                  checked mode) and scores of -inf. An entity that occurs more
  *                  than once has the sum of its p
  *   temperature    in [1e-30, 1e30]
- *   row_weight     device float [batch], or NULL (1 for every row)
+ *   row_weight     device float [batch], or NULL (1 for every row). Times
+ *                  temperature at most float32's largest value: beyond it, and
+ *                  where it is NaN, the row's gradient is NaN
  *   out_loss       device float [batch] or NULL (without row_weight)
  *   out_grad       device [batch x n_entities] of dtype, row stride ld_grad, or
  *                  NULL; may be `scores` itself (with the same stride), and must

@@ -262,7 +262,9 @@ __global__ __launch_bounds__(DT, WAVES) void k_distill(DistillArgs a, float chi,
     }
 
     const float w = a.weight ? a.weight[b] : 1.f;
-    const double wt = (double)w * a.tau;
+    // (a factor beyond float32 makes the whole row NaN, not some entries
+    // infinite and the masked ones NaN)
+    const double product = (double)w * a.tau, wt = fabs(product) <= 3.4028234664e38 ? product : __builtin_nan("");
     // a row without a target, or without weight, has no gradient
     const bool zero = empty || w == 0.f;
     const float f = zero ? 0.f : (float)(zt == zt ? wt / Z : zt);

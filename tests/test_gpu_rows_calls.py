@@ -95,3 +95,39 @@ def test_gpu_embed_grad_of_hot_ids_is_exact(eng, n, d, src):
         old = torch.as_tensor(rng.integers(-9, 9, (V, d)), device="cuda").float()
         acc = eng.embed_grad(tg, ti, V, scale=-2.0, out=old.clone(), accumulate=True)
         assert np.array_equal(acc.double().cpu().numpy(), old.double().cpu().numpy() - 2.0 * want[:V]), kind
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("N", [300, 20001, 66001])
+def test_gpu_distill_weights_at_the_end_of_float32(N, dtype):
+    """A weight times the temperature up to float32's largest value gives the
+    gradient, with zeros where entities are masked; one beyond it, an infinite
+    one or a NaN makes the row's gradient NaN; a row without a target or of
+    weight 0 has none."""
+    import torch
+    eng = kgq.Engine(kgq.GQE, N, 1, 4, 24.0, 1)
+    rng = np.random.default_rng(N)
+    B = 8
+    z = rng.normal(0, 1, (B, N)).astype(np.float32)
+    z[:, 5::3] = -np.inf
+    idx = np.tile(np.int32([0, 1, 3]), (B, 1))
+    t = rng.normal(0, 1, (B, 3)).astype(np.float32)
+    idx[6] = -1
+    w = np.float32([1.0, 1.6e38, -1.6e38, 3e38, np.inf, np.nan, np.inf, 0.0])
+    c = lambda a: torch.as_tensor(a, device="cuda")
+    tz = c(z).to(getattr(torch, dtype))
+    loss, grad = eng.distill(tz, c(idx), c(t), temperature=2.0, weight=c(w))
+    plain = eng.distill(tz, c(idx), c(t), temperature=2.0)
+    assert torch.equal(loss, plain[0])
+    assert grad[3:6].isnan().all() and not grad[6:].any()
+    one = eng.distill(tz[1:3].float(), c(idx[1:3]), c(t[1:3]), temperature=2.0)[1].double()
+    for row in (1, 2):
+        assert torch.isfinite(grad[row]).all() and not grad[row, 5::3].any()
+        want = one[row - 1] * float(w[row])
+        # float32's weight-1 gradient and this one, each with 4 roundings of 2^-24 or less, then bfloat16's
+        tol = 2.0 ** -21 + (2.0 ** -8 if dtype == "bfloat16" else 0.0)
+        listed = torch.zeros(N, dtype=torch.bool, device="cuda")
+        listed[c(idx[1]).long()] = True
+        assert ((grad[row].double() - want).abs() <= tol * want.abs())[~listed].all()
+        # (a listed entity's is a difference of two shares, each at most 1)
+        assert ((grad[row].double() - want).abs() <= tol * want.abs() + 2.0 ** -21 * 2 * 1.6e38)[listed].all()
