@@ -1089,7 +1089,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
     float skip = cut ? ranking_score(cut) : -INFINITY;
     if (!by_mass && min_p > 0.0) {
         const double low = (double)M + set.temperature * (log(min_p) - 1e-6) - fabs((double)M) * 1e-6;
-        skip = fmaxf(skip, (float)fmax(low, -3e38));
+        if (low > -3.4028234664e38) skip = fmaxf(skip, (float)low);      // (else no score lies below it)
     }
     double z = 0.0, above = 0.0;
     // (whether the wavefront has anything to sum; sum: a lane's)
