@@ -504,7 +504,8 @@ typedef struct {
 } kgq_sampling;
 
 /* Device bytes of workspace for a kgq_sample of this batch (0 for n_entities
- * above 327,680). Errors: INVALID_ARG (NULL argument, batch outside [1, 2^20]). */
+ * above 327,680), whatever its settings (a call that cuts nothing uses them).
+ * Errors: INVALID_ARG (NULL argument, batch outside [1, 2^20]). */
 kgq_status kgq_sample_workspace(const kgq_handle* h, int32_t batch, size_t* bytes);
 
 /* Draw n_draws entities for each row of scores, with replacement, from given

@@ -68,12 +68,14 @@ __device__ __forceinline__ float word_value(const W& w, int e)
 // scores' place, or (KEEP false, bfloat16: half the registers, and twice the
 // rows in flight) are computed again for the gradient. NV = 0: the row is read
 // twice. Three barriers: behind the maxima, the sums, and the row's stores.
-// Bound by memory where rows are many: 2,048 rows of 63,361, K = 100: 237 us,
-// 4.4 TB/s read and written (a plain copy of the scores 195 us: it has no
-// barrier between its loads and its stores, and more than one row a compute
-// unit to fill the gaps). 1,024 in bfloat16, K = 1,000: 98 us, 2.6 TB/s, where
-// the exponentials, two a score, take as long as the bytes. 509 rows of 14,505:
-// 15.7 us, 3.8 TB/s. 32 rows of 1,000: 6 us, the latency of the three barriers.
+// Bound by memory where rows are many: 2,048 rows of 63,361, K = 100: 237 us a
+// call among others (243 as profiled), 4.4 TB/s read and written (a plain copy of
+// the scores 195 us: it has no barrier between its loads and its stores, and more
+// than one row a compute unit to fill the gaps). 1,024 in bfloat16, K = 1,000: 98
+// us (95), 2.6 TB/s, where the exponentials, two a score, take as long as the
+// bytes. 509 rows of 14,505: 15 us (15.8), 4.0 TB/s. 32 rows of 1,000: 6 us as
+// profiled, the latency of the three barriers. The loss alone of 2,048 rows: 150
+// us, 3.5 TB/s read; 500 rows of 200,000, read twice: 250 us.
 template <typename T, int DT, int NV, bool KEEP, int WAVES>
 __global__ __launch_bounds__(DT, WAVES) void k_distill(DistillArgs a, float chi, float clo, int slots)
 {

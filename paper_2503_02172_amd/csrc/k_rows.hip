@@ -306,7 +306,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(EmbedGradArgs a, co
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     {
         // each digit's keys, and those in the blocks before this one: a
-        // wavefront per block's histogram, 16 loads at most, all in flight
+        // wavefront per block's histogram, 8 loads at most, all in flight
         uint4 all4 = make_uint4(0, 0, 0, 0), before4 = all4;
 #pragma unroll
         for (int k = 0; k < kSortBlocks / kSortWaves; ++k) {
@@ -527,8 +527,9 @@ __device__ __forceinline__ void add_pieces(const float* rest, int d, int lo, int
 // pieces in chunk order. A wavefront looks at one chunk and adds a run of few
 // pieces by itself; the workgroup then takes the longer runs of its 16 chunks
 // together (each wavefront a share of the pieces, the shares added in order).
-// 262,144 tokens, log-uniform ids: 13 us (the whole gradient 160; 203 if the
-// workgroup takes every run); of few chunks 6 us, a chain of four loads.
+// 262,144 tokens, log-uniform ids: 13 us (the whole call 157; 200 if the
+// workgroup takes every run); 2,500 tokens 8 us, 64 of one run 6: a chain of
+// four loads.
 template <typename O>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_grad_join(EmbedGradArgs a, GradCut cut, const int32_t* keys,
                                                                const float* piece)
@@ -614,10 +615,10 @@ int sort_blocks(int64_t n)
 
 // Groups of just enough lanes for a row, 16 bytes a lane, and chunks that give
 // the chip some 16 wavefronts a compute unit: 8 to 64 tokens (5,000 tokens of
-// 400: 31 us with 8, 49 with 64; 262,144: 160 us with 64, 228 with 8; longer ones
+// 400: 31 us with 8, 49 with 64; 262,144: 157 us with 64, 225 with 8; longer ones
 // would save pieces, one or two rows a chunk, that are few beside 64 already).
-// The element size is the smaller of the two types', so that the workspace
-// holds either.
+// vec: elements of 16 bytes of the gradient's type; the workspace, which is
+// asked for without it, holds the pieces of either type's cut.
 GradCut grad_cut(int64_t n, int d, int vec)
 {
     GradCut c;
@@ -662,8 +663,9 @@ namespace {
 template <typename T, typename O>
 void launch_all(const EmbedGradArgs& a, hipStream_t s)
 {
-    // One launch instead of six or more: 12 us for 1,536 tokens of 400 and 29
-    // sorted, 61: 8 and 23, 2,500: 17 and 30, 4,096: 26 and 31. But ids with
+    // One launch instead of six or more: a call takes 11 us for 1,536 tokens of
+    // 400 and 28 sorted, 61: 10 (the host's) and 24, 2,500: 17 and 29, 4,096: 26
+    // and 30. But ids with
     // hundreds of tokens take longer than sorted (1,536 of one id: 57 us and 30),
     // and longer the more tokens: hence no more than kFew.
     if (a.n <= kFew) {

@@ -26,7 +26,11 @@
 // sorted, gives the cut exactly, or says that it lies elsewhere. Such rows are
 // left to a second launch (k_sample_far), which narrows the range down by
 // histogram after histogram, counts and fixed-point weights added with integer
-// atomics, whose order does not matter.
+// atomics, whose order does not matter. It starts over, so that such a row
+// takes two to five times as long: infinite scores, more than 2,048 entries in
+// the bins around the cut (bfloat16 scores, which tie, of rows above 65,536, or
+// of any at high temperatures), and a top-k above the number of entries that
+// are not masked.
 #include <algorithm>
 #include <type_traits>
 
@@ -38,7 +42,7 @@ namespace {
 
 constexpr int kBins = 2048;
 constexpr int kSort = 2048;                  // entries that are sorted for a cut
-constexpr int kRankSort = 512;               // of these, sorted by counting (top-p, 2,048 rows: 379 us, 404 by merging)
+constexpr int kRankSort = 512;               // of these, sorted by counting (top-p, 2,048 rows, a call: 379 us, 404 by merging)
 constexpr int kDrawn = 1024;                 // draws of a row whose logarithms are taken together
 constexpr int kRun = 16;                     // lanes per draw, and per 64 scores
 constexpr int kPiece = 1024;                 // scores of a row per wavefront, without cuts
@@ -191,8 +195,8 @@ __device__ __forceinline__ V block_scan(V x, V* buf, V* total)
 
 // The bin of the histogram at which the goal is met, and what the bins before
 // it hold (added to *count / *mass). weight_of: what a bin's fixed-point sum
-// is counted in. false: the goal lies behind every bin (the last bin with an
-// entry is then taken).
+// is counted in. Where the goal lies behind every bin, the last one with an
+// entry is taken.
 template <int THREADS, int CHUNKS, typename W>
 __device__ __forceinline__ void find_bin(SampleLds<THREADS, CHUNKS>& L, const CutGoal& goal, W weight_of, uint32_t* count,
                                          double* mass)
@@ -866,14 +870,16 @@ __device__ __forceinline__ void draw_kept(SampleLds<THREADS, CHUNKS>& L, const S
 // One workgroup per row. NV > 0: the row's scores in registers, NV vectors of
 // four a thread, element (j THREADS + thread) 4 + e; NV = 0: read again in each
 // pass.
-// 2,048 rows of 63,361, top-p 0.9: 388 us, 1.3 TB/s. A row takes about 42 us of
+// 2,048 rows of 63,361, top-p 0.9: 387 us as profiled, 1.3 TB/s (a call among
+// others, with the second launch, 378). A row takes about 42 us of
 // its compute unit, one row after the other: loading 6, largest score 1,
 // histogram 7, its bins 2, the pass in doubles 18, list and cut 3, the draw
 // 3.5. So the phases' latency bounds it, and the doubles, which cost 18 us a row
 // here and bound the sums without cuts at 16. (256 of the 512 registers of a
 // lane hold scores: a second row does not fit; 1,024 threads with half as many
-// each spill.) top-k 100: 284 us, min-p 160. 61 rows with all cuts: 59 us, and
-// one row of 14,505 with top-p 20: the latency of the phases alone.
+// each spill.) top-k 100: 292 us, min-p 0.02 156; bfloat16 rows, held as
+// float32, take 407, 263 and 130. 61 rows with all cuts: 59 us, and one row of
+// 14,505 with top-p 20: the latency of the phases alone.
 template <typename T, int THREADS, int NV, int CHUNKS, int WAVES>
 __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
 {
@@ -1183,7 +1189,9 @@ __global__ __launch_bounds__(THREADS, WAVES) void k_sample_rows(SampleArgs a)
 // The rows that k_sample_rows left: infinite scores, more equal or nearly
 // equal scores around a cut than it sorts, a cut it did not find. One
 // workgroup per row, which is read once for each step of the search. 4 us where
-// there is no such row.
+// there is no such row; 2,048 rows of 63,361 with 50 entries that are not masked
+// and top-k 100: 650 us; 500 bfloat16 rows of 200,000, top-p 0.9 at temperature
+// 1.5, all of them left: 1,450 us.
 template <typename T>
 __global__ __launch_bounds__(512) void k_sample_far(SampleArgs a)
 {
