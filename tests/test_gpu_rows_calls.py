@@ -131,3 +131,73 @@ def test_gpu_distill_weights_at_the_end_of_float32(N, dtype):
         assert ((grad[row].double() - want).abs() <= tol * want.abs())[~listed].all()
         # (a listed entity's is a difference of two shares, each at most 1)
         assert ((grad[row].double() - want).abs() <= tol * want.abs() + 2.0 ** -21 * 2 * 1.6e38)[listed].all()
+
+
+def test_gpu_embed_grad_copies_in_a_captured_graph(eng):
+    """A gradient that has to be copied, captured: every replay copies what it
+    holds then."""
+    import torch
+    V, T, n, d = 70, 6, 500, 20
+    base = torch.zeros(n, T, d, device="cuda")
+    ids = torch.zeros(T, n, dtype=torch.int32, device="cuda")
+    grad = base.transpose(0, 1)
+    eng.embed_grad(grad, ids, V)
+    torch.cuda.synchronize()
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        out = eng.embed_grad(grad, ids, V)
+    for turn in range(3):
+        base.copy_(torch.as_tensor(odd_rows(n * T, d, turn).reshape(n, T, d)))
+        ids.copy_(torch.as_tensor(np.random.default_rng(turn).integers(-1, V, (T, n)).astype(np.int32)))
+        eager = eng.embed_grad(grad, ids, V)
+        gr.replay()
+        torch.cuda.synchronize()
+        want = np.zeros((V + 1, d))
+        np.add.at(want, ids.cpu().numpy().ravel(), grad.double().cpu().numpy().reshape(-1, d))
+        assert torch.equal(out, eager) and np.array_equal(out.double().cpu().numpy(), want[:V]), turn
+
+
+def test_gpu_largest_counts(eng):
+    """2^20 rows of scores, tables of 2^31 - 1 rows, and 2^31 - 1 tokens."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 90e9:
+        pytest.skip("needs 60 GB of device memory")
+    B, N = 1 << 20, 37
+    scorer = kgq.Engine(kgq.GQE, N, 1, 4, 24.0, 1)
+    x, u = torch.randn(B, N, device="cuda"), torch.rand(B, 1, device="cuda")
+    idx, score = torch.randint(0, N, (B, 2), device="cuda", dtype=torch.int32), torch.randn(B, 2, device="cuda")
+    some = torch.randint(0, B, (200,), device="cuda")
+    some[0] = B - 1
+    for kw in (dict(), dict(top_p=0.8)):
+        assert torch.equal(scorer.sample(x, u, **kw)[0][some], scorer.sample(x[some], u[some], **kw)[0])
+    for a, b in zip(scorer.distill(x, idx, score), scorer.distill(x[some], idx[some], score[some])):
+        assert torch.equal(a[some], b)
+
+    V = (1 << 31) - 1
+    out = torch.empty(V, 1, device="cuda", dtype=torch.bfloat16)
+    for n in (100, 2048, 5000):
+        print(f"[counts] {V} rows, {n} tokens", flush=True)
+        ids = torch.randint(0, V, (n,), device="cuda", dtype=torch.int32)
+        ids[:4] = torch.tensor([V - 1, 0, -1, V - 1], dtype=torch.int32)
+        out.fill_(3.0)
+        eng.embed_grad(torch.ones(n, 1, device="cuda"), ids, V, out=out)
+        used = sum(int((out[i:i + (1 << 28)] != 0).sum()) for i in range(0, V, 1 << 28))
+        assert used == ids[ids >= 0].unique().numel() and out[V - 1, 0] == 2
+        got = eng.embed(out, ids, dtype=torch.float32)
+        assert got[0, 0] == 2 and got[2, 0] == 0
+    del out
+    torch.cuda.empty_cache()
+
+    n, V = (1 << 31) - 1, 1 << 20
+    print(f"[counts] {n} tokens", flush=True)
+    ids = torch.arange(n, device="cuda", dtype=torch.int32).bitwise_and_(V - 1)
+    got = eng.embed_grad(torch.ones(n, 1, device="cuda", dtype=torch.bfloat16), ids, V)
+    assert (got[:-1] == 2048).all() and got[-1] == 2047
+    torch.cuda.empty_cache()
+    t = torch.arange(V, device="cuda").remainder_(256).bfloat16()[:, None]
+    rows = eng.embed(t, ids)
+    for at in range(0, n, 1 << 28):
+        assert torch.equal(rows[at:at + V], t)
+    assert rows[n - 1, 0] == (n - 1) % 256
+    del ids, rows, got
+    torch.cuda.empty_cache()
